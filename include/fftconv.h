@@ -237,6 +237,63 @@ size_t fftconv_workspace_bytes_backward_filter(const fftconv_plan *plan, int64_t
 int fftconv_backward_filter(const fftconv_plan *plan, const void *u, const void *dy, float *dk, int64_t Nk,
                             int64_t B, int64_t H, int64_t N, void *workspace, void *stream);
 
+/* ---- The layers around a convolution: norm, projections and kept activations
+ *
+ * A gated long-convolution layer is a norm of the residual stream, a projection to u, w and v, the gated convolution and a projection
+ * back.  These calls are what stands around the convolution, for training (norm with its gradients, activations kept in 8 bits, the
+ * gradient of a projection's weight) and for serving (norm with 8-bit rows, 8-bit projections, down to single tokens).  They take no
+ * plan; the conventions are those at the top: device pointers, asynchronous on `stream`, nothing allocated, no synchronisation, a code
+ * returned, nothing launched on error.  Tensors need only the alignment of their element type (16 bytes is faster), and no output
+ * overlaps an input.  Sums, statistics and scales are fp32 or 32-bit integers; every value is rounded once, to nearest even, where it is
+ * written.  Results do not depend on timing: every sum has an order that the sizes alone decide.
+ *
+ * 8-bit values: q = x / s rounded to the nearest integer, ties to even, with s = max |x| / 127 over the values that share the scale, so
+ * q is in [-127, 127] (-128 is accepted where 8-bit values are read).  Where max |x| is below 2^-100, s and q are 0.  Where a value is
+ * not finite, s is NaN and q is 0: what is read back is NaN throughout, never a number.
+ *
+ * fftconv_rms_norm: T rows of D values (1 <= D <= 16384; T >= 0),
+ *     h = x + residual,  y = h / sqrt(mean(h^2) + eps) * weight.
+ *   residual may be NULL (h = x).  ldx, ldr: distance between rows of x and of the residual in elements, >= D.  weight: D fp32.  y, h:
+ *   contiguous; h (the residual stream for the next layer, rounded to dtype; the norm is taken of the sum before that) and rstd (T
+ *   fp32, for the backward pass) may be NULL.  scale: NULL, and y is in dtype; or T fp32, and y is in 8 bits with a scale for each row.
+ * fftconv_rms_norm_backward: with z = h rstd and g = dy . weight
+ *     dx = dh + rstd (g - z mean(g z)),  dweight = sum over rows of dy . z.
+ *   dx is the gradient of x and of the residual alike; dh (contiguous, may be NULL) is what comes back along the residual stream; lddy:
+ *   distance between rows of dy.  workspace: fftconv_workspace_bytes_rms_norm_backward bytes (may be NULL when that is 0).
+ * fftconv_quantize_rows: T rows in 8 bits with a scale each, no norm (a projection's weight, rows that come from elsewhere). */
+int fftconv_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const float *weight, void *y, void *h, float *rstd,
+                     float *scale, int64_t T, int64_t D, double eps, int dtype, void *stream);
+size_t fftconv_workspace_bytes_rms_norm_backward(int64_t T, int64_t D, int dtype);
+int fftconv_rms_norm_backward(const void *dy, int64_t lddy, const void *h, const void *dh, const float *weight, const float *rstd, void *dx,
+                              float *dweight, int64_t T, int64_t D, int dtype, void *workspace, void *stream);
+int fftconv_quantize_rows(const void *x, int64_t ldx, int8_t *q, float *scale, int64_t T, int64_t D, int dtype, void *stream);
+
+/* Projection in 8 bits: for the tokens t = (b, n) of B sequences of N samples
+ *     y[t, o] = (sum over k of x[t, k] w[o, k]) x_scale[t] w_scale[o] + bias[o],
+ * the sum in 32-bit integers, exact.  x: (B, N, K), w: (O, K), contiguous; bias: O fp32 or NULL; 1 <= K <= 131071; B N and O below 2^31.
+ *   parts = 0: y is (B, N, O), token by token.  parts >= 1, a divisor of O: y is (parts, B, O / parts, N), channel by channel, what the
+ *   convolutions take: with parts = 3, u, w and v of fftconv_forward_gated lie one after the other.  dtype: of y.
+ *   workspace: fftconv_workspace_bytes_linear_i8 bytes (may be NULL when that is 0). */
+size_t fftconv_workspace_bytes_linear_i8(int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype);
+int fftconv_linear_i8(const int8_t *x, const float *x_scale, const int8_t *w, const float *w_scale, const float *bias, void *y, int64_t B,
+                      int64_t N, int64_t K, int64_t O, int64_t parts, int dtype, void *workspace, void *stream);
+
+/* Activations kept for the backward pass in 8 bits (half of 16-bit ones): q is (B, C, N), the layout of u and y above, and scale
+ * (B, C, ceil(N / 128)) fp32, one for every 128 samples of a channel.
+ * fftconv_act_pack: from x, (B, C, N), or (B, N, C) with tokens = 1.
+ * fftconv_act_unpack: x[b, c, n] = q s, or its product with a second one, (q s)(gate_q gate_scale), or with a tensor `gate` in dtype
+ *   (what the gradients of a gated convolution take: u . w for fftconv_backward_filter).  gate_q with gate_scale, or gate, or none.
+ * fftconv_linear_grad_weight: the gradient of a projection's weight from its kept input,
+ *     dw[o, c] = sum over b, n of dy[b, n, o] q[b, c, n] scale[b, c, n / 128].
+ *   dy: (B, N, O) with tokens = 1, else (B, O, N).  dw: (O, C), fp32 or dtype (dtype_dw).  B ceil(N / 128), O and C below 2^31.
+ *   Products are exact (8-bit values times dy), sums in fp32.  workspace: fftconv_workspace_bytes_linear_grad_weight bytes. */
+int fftconv_act_pack(const void *x, int8_t *q, float *scale, int64_t B, int64_t C, int64_t N, int tokens, int dtype, void *stream);
+int fftconv_act_unpack(const int8_t *q, const float *scale, const int8_t *gate_q, const float *gate_scale, const void *gate, void *x, int64_t B,
+                       int64_t C, int64_t N, int dtype, void *stream);
+size_t fftconv_workspace_bytes_linear_grad_weight(int64_t B, int64_t N, int64_t O, int64_t C, int tokens, int dtype);
+int fftconv_linear_grad_weight(const void *dy, const int8_t *q, const float *scale, void *dw, int64_t B, int64_t N, int64_t O, int64_t C,
+                               int tokens, int dtype, int dtype_dw, void *workspace, void *stream);
+
 /* Fraction of k_f that a cut-off pattern zeroes (Appendix A.4): k_f is viewed
  * as an ndim-dimensional array of shape dims[0..ndim) and, in every dimension
  * i, the last cuts[i] indices are set to zero (cuts[i] = how much of that

@@ -1,0 +1,109 @@
+// What the kernels around the convolutions share (row_norm.hip, linear_i8.hip, checkpoint.hip, weight_grad.hip): I/O types, loads and
+// stores of any alignment, reductions over a wave.
+#pragma once
+
+#include "fftconv_internal.h"
+
+namespace fftconv {
+namespace lay {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(16))) int i32x16;
+
+// Rows and runs whose largest magnitude is below 2^-100 are zeros with a scale of zero: their scale would come near the subnormal
+// numbers, where its own rounding is no longer small.
+constexpr float LEAST = 0x1p-100f;
+constexpr int RUN = 128;                                      // samples of a channel that share a scale in a checkpoint
+
+template <typename T> struct Vec8 { T v[8]; };
+
+template <typename T> __device__ __forceinline__ float to_f32(T x) { return (float)x; }
+template <typename T> __device__ __forceinline__ T from_f32(float x) { return (T)x; }      // round to nearest even
+
+// E values from p, of which the first `left` are there (the others read as zero). A whole piece is one load of E * sizeof(T) bytes at any
+// alignment of T.
+template <typename T, int E> __device__ __forceinline__ void load_piece(const T *p, int64_t left, float (&v)[E])
+{
+    if (left >= E) {
+        T raw[E];
+        __builtin_memcpy(raw, p, sizeof(raw));
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = to_f32(raw[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = e < left ? to_f32(p[e]) : 0.f;
+    }
+}
+
+template <typename T, int E> __device__ __forceinline__ void store_piece(T *p, int64_t left, const T (&raw)[E])
+{
+    if (left >= E) {
+        __builtin_memcpy(p, raw, sizeof(raw));
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < left) p[e] = raw[e];
+    }
+}
+
+template <typename T, int E> __device__ __forceinline__ void store_rounded(T *p, int64_t left, const float (&v)[E])
+{
+    T raw[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) raw[e] = from_f32<T>(v[e]);
+    store_piece<T, E>(p, left, raw);
+}
+
+// A magnitude as an integer: of two, the larger number is the larger integer, infinities are above every finite number and NaN above
+// infinities, so the largest of a row says whether anything in it is not finite.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+
+// Reduction over groups of 16 lanes, or over the wave, every lane ending with the result: exchanges inside the vector unit (lane pairs, quads,
+// half rows and rows of 16, then rows and halves of the wave swapped), no trip through LDS. The order of the additions is fixed.
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+template <typename F> __device__ __forceinline__ uint32_t reduce16(uint32_t x, F f)
+{
+    x = f(x, dpp<0xB1>(x));       // lanes ^ 1
+    x = f(x, dpp<0x4E>(x));       // lanes ^ 2
+    x = f(x, dpp<0x141>(x));      // the other quad of the half row
+    x = f(x, dpp<0x140>(x));      // the other half of the row
+    return x;
+}
+template <typename F> __device__ __forceinline__ uint32_t reduce64(uint32_t x, F f)
+{
+    x = reduce16(x, f);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f(r[0], r[1]);
+    const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return f(h[0], h[1]);
+}
+struct AddF32 {
+    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+    }
+};
+struct MaxU32 {
+    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
+};
+__device__ __forceinline__ float wave_sum(float x) { return __builtin_bit_cast(float, reduce64(__builtin_bit_cast(uint32_t, x), AddF32())); }
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) { return reduce64(x, MaxU32()); }
+
+// Scale of values whose largest magnitude has these bits: max / 127; zero for values below LEAST; NaN where a value is not finite, so that
+// nothing read back from 8 bits passes for a number that was there.
+__device__ __forceinline__ float scale_of(uint32_t top)
+{
+    const float m = __builtin_bit_cast(float, top);
+    return top >= 0x7f800000u ? __builtin_nanf("") : m < LEAST ? 0.f : m / 127.f;
+}
+// q = x / s rounded to the nearest integer, ties to even; the division is rounded as IEEE 754 has it, so that q is a function of x and s
+// alone. Zero where the scale is zero or NaN.
+__device__ __forceinline__ int8_t quantised(float x, float s) { return s > 0.f ? (int8_t)(int)rintf(x / s) : (int8_t)0; }
+
+}  // namespace lay
+}  // namespace fftconv

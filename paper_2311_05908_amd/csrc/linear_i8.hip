@@ -1,0 +1,295 @@
+// Product of rows in 8 bits with a weight in 8 bits, a scale for each token and for each output channel:
+//
+//   y[t, o] = (sum over k of x[t, k] w[o, k]) xs[t] ws[o] + bias[o]        the sum in 32-bit integers, exact; one rounding, at the store
+//
+// One kernel serves both layouts of y. Its two operands, both with k contiguous, are R, whose rows lie next to each other in y, and S:
+// token by token (t, o) R is the weight, channel by channel (parts, b, o / parts, n) R is the tokens. An accumulator of the matrix cores holds
+// four consecutive rows of R for one row of S in a lane, so the values that a lane stores are neighbours in y either way.
+#include "layers_internal.h"
+
+namespace fftconv {
+namespace lay {
+
+struct LinArgs {
+    const int8_t *r, *s;          // (nr, K), (ns, K)
+    const float *rscale, *sscale, *rbias, *sbias;
+    void *y;
+    int64_t K;
+    int nr, ns;
+    int channels;                 // y channel by channel: R is b * N + n, S is o
+    int N, per_part;              // samples of a sequence; output channels of a part
+    int64_t B;
+    int tiles_r, tiles_s;
+};
+
+// First value of y in row s of S: y[column(s) + offset(r)].
+__device__ __forceinline__ int64_t column_of(const LinArgs &a, int s)
+{
+    if (!a.channels) return (int64_t)s * a.nr;
+    const int part = s / a.per_part;
+    return ((int64_t)part * a.B * a.per_part + (s - part * a.per_part)) * a.N;
+}
+// ... and the place of row r of R in it.
+__device__ __forceinline__ int64_t row_of(const LinArgs &a, int r)
+{
+    if (!a.channels) return r;
+    const int b = r / a.N;
+    return (int64_t)b * a.per_part * a.N + (r - b * a.N);
+}
+
+template <int FR, int FS> struct Tile {
+    static constexpr int BR = 64 * FR, BS = 64 * FS, BK = 64;      // 2 x 2 waves of FR x FS accumulators of 32 x 32
+    static constexpr int STAGE = (BR + BS) * BK;
+};
+
+// The place in LDS of 16-byte piece c (0 .. 3) of a 64-byte row: two rows share the 128 bytes that a clock delivers, and eight lanes with
+// consecutive rows read the same piece at once, so the piece is moved by bits 1 and 2 of the row: all eight come from banks of their own.
+__device__ __forceinline__ int piece_at(int row, int c) { return row * 64 + ((c ^ ((row >> 1) & 3)) << 4); }
+
+// 16 bytes of a row of K from column k on; what lies beyond K reads as zero.
+__device__ __forceinline__ uint4 load16(const int8_t *row, int64_t k, int64_t K)
+{
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (k + 16 <= K) {
+        __builtin_memcpy(&v, row + k, 16);
+    } else if (k < K) {
+        uint32_t w[4] = {};
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (k + e < K) w[e / 4] |= (uint32_t)(uint8_t)row[k + e] << (8 * (e % 4));
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return v;
+}
+
+__device__ __forceinline__ i32x16 mfma_i8(uint4 a, uint4 b, i32x16 c)
+{
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+
+// W values of y in row s of S, from row r of R on (r a multiple of W).
+template <typename T, int W> __device__ __forceinline__ void put(const LinArgs &a, int64_t col, int r, const T (&v)[W])
+{
+    T *const y = (T *)a.y + col;
+    if (r + W <= a.nr && (!a.channels || r % a.N + W <= a.N)) {
+        __builtin_memcpy(y + row_of(a, r), v, sizeof(v));
+    } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            if (r + e < a.nr) y[row_of(a, r + e)] = v[e];
+    }
+}
+
+// One accumulator of 32 x 32: lane l holds column l % 32, register i row 8 (i / 4) + 4 (l / 32) + i % 4.
+template <typename T> __device__ __forceinline__ void epilogue(const LinArgs &a, const i32x16 &acc, int r0, int s, const float (&rs)[16],
+                                                               const float (&rb)[16], float ss, float sb, int64_t col)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = fmaf((float)acc[i] * rs[i], ss, rb[i] + sb);
+    if constexpr (sizeof(T) == 4) {
+        if (s >= a.ns) return;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float o[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+            put<float, 4>(a, col, r0 + 8 * j + 4 * half, o);
+        }
+    } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const T p[2] = {from_f32<T>(v[2 * i]), from_f32<T>(v[2 * i + 1])};
+            __builtin_memcpy(&w[i], p, 4);
+        }
+        // rows 8 j + 4 half ... + 3 of two j: the halves of the wave exchange, so that each lane has eight rows in a run
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const auto x = __builtin_amdgcn_permlane32_swap(w[2 * j + i], w[2 * j + 2 + i], false, false);
+                o[i] = x[0], o[i + 2] = x[1];
+            }
+            T t[8];
+            __builtin_memcpy(t, o, 16);
+            if (s < a.ns) put<T, 8>(a, col, r0 + 8 * j + 8 * half, t);
+        }
+    }
+}
+
+template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) k_linear(const LinArgs a)
+{
+    using G = Tile<FR, FS>;
+    constexpr int PIECES = (G::BR + G::BS) * 4 / 256;             // 16-byte pieces a thread stages
+    __shared__ __align__(16) char lds[2 * G::STAGE];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wr = wave >> 1, wsv = wave & 1;
+    const int tr = blockIdx.x / a.tiles_s, ts = blockIdx.x % a.tiles_s;
+    const int r0 = tr * G::BR, s0 = ts * G::BS;
+    const int8_t *src[PIECES];
+    int dst[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = threadIdx.x + i * 256, row = p >> 2, c = p & 3;
+        const bool is_r = row < G::BR;
+        const int g = is_r ? min(r0 + row, a.nr - 1) : min(s0 + row - G::BR, a.ns - 1);      // rows beyond the end: the last one, not stored
+        src[i] = (is_r ? a.r : a.s) + (int64_t)g * a.K;
+        dst[i] = piece_at(row, c);
+    }
+    uint4 stage[PIECES];
+    const int steps = (int)((a.K + G::BK - 1) / G::BK);
+    auto fetch = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) stage[i] = load16(src[i], (int64_t)step * G::BK + (threadIdx.x & 3) * 16, a.K);
+    };
+    auto keep = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) *(uint4 *)(lds + buf * G::STAGE + dst[i]) = stage[i];
+    };
+    i32x16 acc[FR][FS] = {};
+    fetch(0);
+    keep(0);
+    lds_barrier();
+    const int half = lane >> 5, l32 = lane & 31;
+    for (int k = 0; k < steps; ++k) {
+        if (k + 1 < steps) fetch(k + 1);
+        const char *const base = lds + (k & 1) * G::STAGE;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            uint4 fr[FR], fs[FS];
+#pragma unroll
+            for (int i = 0; i < FR; ++i) fr[i] = *(const uint4 *)(base + piece_at((wr * FR + i) * 32 + l32, kk * 2 + half));
+#pragma unroll
+            for (int i = 0; i < FS; ++i) fs[i] = *(const uint4 *)(base + piece_at(G::BR + (wsv * FS + i) * 32 + l32, kk * 2 + half));
+#pragma unroll
+            for (int i = 0; i < FR; ++i)
+#pragma unroll
+                for (int j = 0; j < FS; ++j) acc[i][j] = mfma_i8(fr[i], fs[j], acc[i][j]);
+        }
+        if (k + 1 < steps) {
+            keep((k + 1) & 1);
+            lds_barrier();
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < FR; ++i) {
+        const int rbase = r0 + (wr * FR + i) * 32;
+        float rs[16], rb[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = min(rbase + 8 * (e / 4) + 4 * half + e % 4, a.nr - 1);
+            rs[e] = a.rscale[r];
+            rb[e] = a.rbias ? a.rbias[r] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < FS; ++j) {
+            const int s = s0 + (wsv * FS + j) * 32 + l32, sc = min(s, a.ns - 1);
+            epilogue<T>(a, acc[i][j], rbase, s, rs, rb, a.sscale[sc], a.sbias ? a.sbias[sc] : 0.f, column_of(a, sc));
+        }
+    }
+}
+
+// Few tokens (S, up to 16 NT of them): what counts is how fast the weight streams in, so its rows go from memory straight into the
+// operand registers, sixteen rows to a workgroup, whose waves divide k among themselves and add their sums up in LDS.
+struct FewArgs {
+    const int8_t *x, *w;
+    const float *xs, *ws, *bias;
+    void *y;
+    int64_t K, B;
+    int T, O, channels, N, per_part;
+};
+
+template <typename T, int NT> __global__ void __launch_bounds__(512) k_linear_few(const FewArgs a)
+{
+    __shared__ i32x4 sums[8][NT][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
+    const int o0 = blockIdx.x * 16;
+    const int8_t *const w = a.w + (int64_t)min(o0 + l16, a.O - 1) * a.K;
+    const int8_t *x[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) x[j] = a.x + (int64_t)min(j * 16 + l16, a.T - 1) * a.K;
+    i32x4 acc[NT] = {};
+    constexpr int U = NT == 1 ? 4 : 2;
+    for (int64_t k0 = (int64_t)wave * 64; k0 < a.K; k0 += 512 * U) {
+        uint4 fw[U], fx[U][NT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t k = k0 + 512 * u + quarter * 16;
+            fw[u] = load16(w, k, a.K);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fx[u][j] = load16(x[j], k, a.K);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, fw[u]), __builtin_bit_cast(i32x4, fx[u][j]), acc[j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sums[wave][j][lane] = acc[j];
+    lds_barrier();
+    // lane l holds token l % 16 of the sixteen, outputs 4 (l / 16) ... + 3
+    for (int i = threadIdx.x; i < NT * 256; i += 512) {
+        const int e = i & 3, l = (i >> 2) & 63, j = i >> 8;
+        int sum = 0;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) sum += sums[v][j][l][e];
+        const int t = j * 16 + (l & 15), o = o0 + 4 * (l >> 4) + e;
+        if (t >= a.T || o >= a.O) continue;
+        const float v = fmaf((float)sum * a.ws[o], a.xs[t], a.bias ? a.bias[o] : 0.f);
+        int64_t at = (int64_t)t * a.O + o;
+        if (a.channels) {
+            const int part = o / a.per_part, b = t / a.N;
+            at = ((((int64_t)part * a.B + b) * a.per_part) + (o - part * a.per_part)) * a.N + (t - b * a.N);
+        }
+        ((T *)a.y)[at] = from_f32<T>(v);
+    }
+}
+
+template <typename T> static int run(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, void *y, int64_t B,
+                                     int64_t N, int64_t K, int64_t O, int64_t parts, hipStream_t s)
+{
+    const int64_t t = B * N;
+    if (t <= 64) {
+        const FewArgs a = {xq, wq, xs, ws, bias, y, K, B, (int)t, (int)O, parts > 0, (int)N, (int)(parts ? O / parts : O)};
+        const unsigned g = (unsigned)((O + 15) / 16);
+        if (t <= 16) k_linear_few<T, 1><<<g, 512, 0, s>>>(a);
+        else if (t <= 32) k_linear_few<T, 2><<<g, 512, 0, s>>>(a);
+        else k_linear_few<T, 4><<<g, 512, 0, s>>>(a);
+        FC_HIP(hipGetLastError());
+        return FFTCONV_OK;
+    }
+    LinArgs a = {};
+    a.channels = parts > 0;
+    a.r = a.channels ? xq : wq, a.s = a.channels ? wq : xq;
+    a.rscale = a.channels ? xs : ws, a.sscale = a.channels ? ws : xs;
+    (a.channels ? a.sbias : a.rbias) = bias;
+    a.y = y, a.K = K, a.nr = (int)(a.channels ? t : O), a.ns = (int)(a.channels ? O : t);
+    a.N = (int)N, a.per_part = (int)(parts ? O / parts : O), a.B = B;
+    auto launch = [&](auto fr, auto fs) -> int {
+        constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value;
+        using G = Tile<FR, FS>;
+        a.tiles_r = (a.nr + G::BR - 1) / G::BR, a.tiles_s = (a.ns + G::BS - 1) / G::BS;
+        k_linear<T, FR, FS><<<(unsigned)((int64_t)a.tiles_r * a.tiles_s), 256, 0, s>>>(a);
+        FC_HIP(hipGetLastError());
+        return FFTCONV_OK;
+    };
+    auto tiles = [&](int br, int bs) { return (int64_t)((a.nr + br - 1) / br) * ((a.ns + bs - 1) / bs); };
+    if (tiles(128, 256) >= 512) return launch(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+    if (tiles(128, 128) >= 256) return launch(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
+    return launch(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+}
+
+size_t linear_i8_workspace(int64_t, int64_t, int64_t, int64_t) { return 0; }
+
+int linear_i8(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, void *y, int64_t B, int64_t N, int64_t K,
+              int64_t O, int64_t parts, int dtype, void *, hipStream_t s)
+{
+    if (dtype == FFTCONV_BF16) return run<__bf16>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, s);
+    if (dtype == FFTCONV_F16) return run<_Float16>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, s);
+    return run<float>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, s);
+}
+
+}  // namespace lay
+}  // namespace fftconv

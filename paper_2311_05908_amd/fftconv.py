@@ -28,6 +28,9 @@ EXPORTS = [
     "fftconv_backward_filter", "fftconv_machine_preset", "fftconv_cost_model", "fftconv_balanced_factors",
     "fftconv_plan_order", "fftconv_filter_fft_sparse_digits", "fftconv_forward_freq_sparse_digits",
     "fftconv_forward_static", "fftconv_plan_create_path", "fftconv_measure_machine",
+    "fftconv_rms_norm", "fftconv_workspace_bytes_rms_norm_backward", "fftconv_rms_norm_backward", "fftconv_quantize_rows",
+    "fftconv_workspace_bytes_linear_i8", "fftconv_linear_i8", "fftconv_act_pack", "fftconv_act_unpack",
+    "fftconv_workspace_bytes_linear_grad_weight", "fftconv_linear_grad_weight",
 ]
 
 STATIC_WORKSPACE_BYTES = 64 << 20      # FFTCONV_STATIC_WORKSPACE_BYTES
@@ -123,6 +126,20 @@ def load(path: str | None = None):
     lib.fftconv_plan_factors.restype = ci
     lib.fftconv_strerror.argtypes = [ci]
     lib.fftconv_strerror.restype = ctypes.c_char_p
+    dbl, size = ctypes.c_double, ctypes.c_size_t
+    for name, result, arguments in (      # the layers around a convolution (layers.py)
+        ("fftconv_rms_norm", ci, [vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, i64, dbl, ci, vp]),
+        ("fftconv_workspace_bytes_rms_norm_backward", size, [i64, i64, ci]),
+        ("fftconv_rms_norm_backward", ci, [vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, ci, vp, vp]),
+        ("fftconv_quantize_rows", ci, [vp, i64, vp, vp, i64, i64, ci, vp]),
+        ("fftconv_workspace_bytes_linear_i8", size, [i64, i64, i64, i64, i64, ci]),
+        ("fftconv_linear_i8", ci, [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, ci, vp, vp]),
+        ("fftconv_act_pack", ci, [vp, vp, vp, i64, i64, i64, ci, ci, vp]),
+        ("fftconv_act_unpack", ci, [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, vp]),
+        ("fftconv_workspace_bytes_linear_grad_weight", size, [i64, i64, i64, i64, ci, ci]),
+        ("fftconv_linear_grad_weight", ci, [vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, ci, vp, vp]),
+    ):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = arguments, result
     lib.fftconv_last_error.argtypes = []
     lib.fftconv_last_error.restype = ctypes.c_char_p
     _libs[path] = lib
