@@ -58,6 +58,10 @@ int check_weight(const char *who, int64_t B, int64_t N, int64_t O, int64_t C, in
     if (!known(dtype)) return bad(who, "unknown dtype");
     if (B < 0 || N < 1 || O < 1 || C < 1 || O > MOST || C > MOST || N > MOST || times(B, (N + 127) / 128) < 0)
         return bad(who, "B >= 0, N, O, C >= 1 are wanted, N, O, C and B ceil(N / 128) below 2^31");
+    if (N > ((int64_t)1 << 22) || O > ((int64_t)1 << 22) || C > ((int64_t)1 << 22)) {        // (distances inside a tile are 32-bit numbers)
+        set_error("%s: sequences of %lld samples, %lld x %lld channels: up to 2^22 are supported", who, (long long)N, (long long)O, (long long)C);
+        return FFTCONV_EUNSUPPORTED;
+    }
     return FFTCONV_OK;
 }
 

@@ -25,8 +25,7 @@ struct WeightArgs {
     const float *scale;
     float *part;                  // (splits, O, C), for the sums of more than one range and for those put aside
     void *dw;
-    int64_t N;
-    int O, C, runs, tiles_c;
+    int sequences, N, O, C, runs, tiles_c, tiles;
     int blocks, per;              // runs of all sequences; of one workgroup
     int splits;
 };
@@ -40,9 +39,9 @@ __device__ __forceinline__ f32x16 mfma16(uint4 a, uint4 b, f32x16 c, _Float16)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// Place in LDS of piece c (8 samples, 16 bytes) of a row of 64: moved by the row, so that neither eight rows in a run (an operand's read) nor
-// eight rows at steps of eight (the write of a transposed piece) meet in one bank.
-__device__ __forceinline__ int place(int row, int c) { return row * 128 + ((c ^ ((row ^ (row >> 3)) & 7)) << 4); }
+// Place in LDS of piece c (8 samples, 16 bytes) of a row of 64: moved by bits 0-2 and 3-4 of the row, so that neither the eight rows that an
+// operand's read takes at once nor the transposed pieces that sixteen lanes write at once meet in a bank.
+__device__ __forceinline__ int place(int row, int c) { return row * 128 + ((c ^ ((row ^ ((row >> 3) & 3)) & 7)) << 4); }
 
 // One 16-bit part after the other of values in T.
 template <typename T, typename P> __device__ __forceinline__ void split(const T &v, P (&o)[Operand<T>::PARTS])
@@ -59,6 +58,27 @@ template <typename T, typename P> __device__ __forceinline__ void split(const T 
     }
 }
 
+// 16 bytes from p, of which the first `left` are wanted and the others read as zero, without reading beyond `end` (the tensor's, which has 16
+// bytes at least): what lies too near the end comes from the last 16 bytes, moved down.
+__device__ __forceinline__ uint4 load_edge(const char *p, const char *end, int64_t left)
+{
+    const char *const from = p + 16 <= end ? p : end - 16;
+    const int64_t off = p - from;
+    unsigned __int128 v;
+    __builtin_memcpy(&v, from, 16);
+    v = left <= 0 ? 0 : v >> (8 * (off < 15 ? off : 15));
+    if (left < 16) v &= ((unsigned __int128)1 << (8 * (left > 0 ? left : 0))) - 1;
+    uint4 r;
+    __builtin_memcpy(&r, &v, 16);
+    return r;
+}
+template <typename T> __device__ __forceinline__ uint4 load_whole(const T *p, uint32_t bytes)
+{
+    uint4 r;
+    __builtin_memcpy(&r, __builtin_assume_aligned((const char *)p + bytes, alignof(T)), 16);
+    return r;
+}
+
 template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void __launch_bounds__(512, 2) k_weight(const WeightArgs a)
 {
     using P = typename Operand<T>::type;
@@ -67,68 +87,74 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
     extern __shared__ __align__(16) char lds[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
     const int wo = wave >> 2, wc = wave & 3;
-    const int o0 = blockIdx.x / a.tiles_c * BO, c0 = blockIdx.x % a.tiles_c * BC;
-    const int first = blockIdx.y * a.per, last = min(first + a.per, a.blocks);
+    // workgroups go to the dies in turn; a die takes neighbouring tiles of one range, which read the same dy and q from its L2
+    const int n_wg = gridDim.x, die = blockIdx.x % 8, spare = n_wg % 8;
+    const int at = die * (n_wg / 8) + min(die, spare) + blockIdx.x / 8;
+    const int tile = at % a.tiles, range = at / a.tiles;
+    const int o0 = tile / a.tiles_c * BO, c0 = tile % a.tiles_c * BC;
+    const int first = range * a.per, last = min(first + a.per, a.blocks);
 
-    constexpr int AV = TOKENS ? (BO * 2 + 511) / 512 : BO * 8 / 512, AK = TOKENS ? 4 : 1;       // pieces of dy a thread stages; rows of a piece
-    constexpr int BV = BC * 4 / 512;
-    // TOKENS: a piece is 8 channels x 4 samples. Bits 0-2 of its number are the channels', so that eight lanes read 128 bytes in a row, and bit 3
-    // the samples', so that sixteen lanes write 128 bytes of different banks.
-    constexpr int OH = BO / 64, OHB = OH == 4 ? 2 : 1;
+    // What a thread stages of 64 samples. dy (b, o, n): pieces of 8 samples, eight to a row. dy (b, n, o): pieces of 8 channels x 4 samples;
+    // bits 0-1 and 4 up of a piece's number are the channels', so that four lanes read 64 bytes in a row, bits 2 and 3 the lowest and the
+    // highest bit of the samples', so that sixteen lanes write 128 bytes of different banks. q: pieces of 16 samples, four to a row.
+    constexpr int AV = TOKENS ? (BO * 2 + 511) / 512 : BO * 8 / 512, AK = TOKENS ? 4 : 1, AW = sizeof(T) / 2, BV = BC * 4 / 512;
+    constexpr int OH = BO / 64, OHB = OH == 4 ? 2 : 1, EA = 16 / sizeof(T);
     static_assert(OH == 4 || OH == 2, "tile");
-    auto group_o = [](int p) { return (p & 7) | ((p >> 4) & (OH - 1)) << 3; };
-    auto group_k = [](int p) { return ((p >> 3) & 1) | (p >> (4 + OHB)) << 1; };
-    T da[AV][AK][8];
-    uint4 db[BV];
-    // step 2 i + h is half h of run first + i
-    auto fetch = [&](int step) {
-        const int blk = first + (step >> 1), b = blk / a.runs, j = blk - b * a.runs;
-        const int64_t n0 = (int64_t)j * RUN + (step & 1) * 64;
+    auto group_o = [](int p) { return (p & 3) | ((p >> 4) & (2 * OH - 1)) << 2; };
+    auto group_k = [](int p) { return ((p >> 2) & 1) | ((p >> (5 + OHB)) & 3) << 1 | ((p >> 3) & 1) << 3; };
+    uint4 da[AV][AK][AW], db[BV];
+    // Distances, in bytes, from the first value of a step's tile. Rows beyond the end are the last one's: what comes of them is not stored.
+    uint32_t aat[AV], bat[BV];
 #pragma unroll
-        for (int i = 0; i < AV; ++i) {
-            const int p = threadIdx.x + i * 512;
-            if constexpr (TOKENS) {
-                if (p >= BO * 2) continue;
-                const int og = group_o(p), kg = group_k(p);
-                const int o = o0 + og * 8;
+    for (int i = 0; i < AV; ++i) {
+        const int p = threadIdx.x + i * 512;
+        if constexpr (TOKENS) aat[i] = ((uint32_t)(group_k(p) * 4) * a.O + (o0 + group_o(p) * 8 < a.O ? group_o(p) * 8 : 0)) * sizeof(T);
+        else aat[i] = ((uint32_t)(min(o0 + (p >> 3), a.O - 1) - o0) * (uint32_t)a.N + (p & 7) * 8) * sizeof(T);
+    }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t n = n0 + kg * 4 + r;
-                    const int left = n < a.N ? a.O - o : 0;
-                    const T *const src = (const T *)a.dy + ((int64_t)b * a.N + n) * a.O + o;
-                    if (left >= 8) {
-                        __builtin_memcpy(da[i][r], src, sizeof(da[i][r]));
-                    } else {
+    for (int i = 0; i < BV; ++i) {
+        const int p = threadIdx.x + i * 512;
+        bat[i] = (uint32_t)(min(c0 + (p >> 2), a.C - 1) - c0) * (uint32_t)a.N + (p & 3) * 16;
+    }
+    // half h of a run
+    auto fetch = [&](int blk, int h) {
+        const int b = blk / a.runs, j = blk - b * a.runs;
+        const int n0 = j * RUN + h * 64;
+        const T *const dy = (const T *)a.dy + (TOKENS ? ((int64_t)b * a.N + n0) * a.O + o0 : ((int64_t)b * a.O + o0) * a.N + n0);
+        const int8_t *const q = a.q + ((int64_t)b * a.C + c0) * a.N + n0;
+        // the last piece of a row of dy may reach into the next row, which the last row does not have
+        const bool edge = n0 + 64 > a.N || (TOKENS && a.O % 8 != 0 && n0 + 64 == a.N);
+        if (!edge) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) da[i][r][e] = e < left ? src[e] : (T)0.f;
-                    }
-                }
-            } else {
-                const int o = o0 + (p >> 3);
-                const int64_t n = n0 + (p & 7) * 8, left = o < a.O ? a.N - n : 0;
-                const T *const src = (const T *)a.dy + ((int64_t)b * a.O + o) * a.N + n;
-                if (left >= 8) {
-                    __builtin_memcpy(da[i][0], src, sizeof(da[i][0]));
-                } else {
+            for (int i = 0; i < AV; ++i) {
+                if (TOKENS && threadIdx.x + i * 512 >= BO * 2) continue;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) da[i][0][e] = e < left ? src[e] : (T)0.f;
-                }
+                for (int r = 0; r < AK; ++r)
+#pragma unroll
+                    for (int w = 0; w < AW; ++w) da[i][r][w] = load_whole(dy + (int64_t)r * a.O + w * EA, aat[i]);
             }
-        }
 #pragma unroll
-        for (int i = 0; i < BV; ++i) {
-            const int p = threadIdx.x + i * 512, c = c0 + (p >> 2);
-            const int64_t n = n0 + (p & 3) * 16, left = c < a.C ? a.N - n : 0;
-            const int8_t *const src = a.q + ((int64_t)b * a.C + c) * a.N + n;
-            db[i] = make_uint4(0, 0, 0, 0);
-            if (left >= 16) {
-                __builtin_memcpy(&db[i], src, 16);
-            } else if (left > 0) {
-                uint32_t w[4] = {};
+            for (int i = 0; i < BV; ++i) db[i] = load_whole(q, bat[i]);
+        } else {
+            const char *const dy_end = (const char *)a.dy + (int64_t)a.sequences * a.O * a.N * (int64_t)sizeof(T);
+            const char *const q_end = (const char *)a.q + (int64_t)a.sequences * a.C * a.N;
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (e < left) w[e / 4] |= (uint32_t)(uint8_t)src[e] << (8 * (e % 4));
-                db[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < AV; ++i) {
+                const int p = threadIdx.x + i * 512;
+                if (TOKENS && p >= BO * 2) continue;
+#pragma unroll
+                for (int r = 0; r < AK; ++r)
+#pragma unroll
+                    for (int w = 0; w < AW; ++w) {
+                        const int o = TOKENS ? group_o(p) * 8 + w * EA : p >> 3, n = TOKENS ? group_k(p) * 4 + r : (p & 7) * 8 + w * EA;
+                        const int64_t left = TOKENS ? (n0 + n < a.N ? a.O - o0 - o : 0) : (o0 + o < a.O ? a.N - n0 - n : 0);
+                        da[i][r][w] = load_edge((const char *)(dy + (TOKENS ? (int64_t)n * a.O + o : (int64_t)o * a.N + n)), dy_end, left * (int)sizeof(T));
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < BV; ++i) {
+                const int p = threadIdx.x + i * 512;
+                db[i] = load_edge((const char *)(q + bat[i]), q_end, a.N - n0 - (p & 3) * 16);
             }
         }
     };
@@ -138,29 +164,35 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
         for (int i = 0; i < AV; ++i) {
             const int p = threadIdx.x + i * 512;
             if constexpr (TOKENS) {
-                const int og = group_o(p), kg = group_k(p);
                 if (p >= BO * 2) continue;
+                const int og = group_o(p), kg = group_k(p);
+                int at = place(og * 8, kg >> 1) + (kg & 1) * 8;          // row og 8 + e: bits 4-6 turned by e
+                asm volatile("" : "+v"(at));                             // (one address kept, not eight)
+                T v[4][8];
+                __builtin_memcpy(v, da[i], sizeof(v));
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     P o[4][NP];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) split<T, P>(da[i][r][e], o[r]);
+                    for (int r = 0; r < 4; ++r) split<T, P>(v[r][e], o[r]);
 #pragma unroll
                     for (int s = 0; s < NP; ++s) {
-                        const P v[4] = {o[0][s], o[1][s], o[2][s], o[3][s]};
-                        __builtin_memcpy(base + s * BO * 128 + place(og * 8 + e, kg >> 1) + (kg & 1) * 8, v, 8);
+                        const P t[4] = {o[0][s], o[1][s], o[2][s], o[3][s]};
+                        __builtin_memcpy(__builtin_assume_aligned(base + s * BO * 128 + e * 128 + (at ^ (e << 4)), 8), t, 8);
                     }
                 }
             } else {
+                T v[8];
+                __builtin_memcpy(v, da[i], sizeof(v));
                 P o[8][NP];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) split<T, P>(da[i][0][e], o[e]);
+                for (int e = 0; e < 8; ++e) split<T, P>(v[e], o[e]);
 #pragma unroll
                 for (int s = 0; s < NP; ++s) {
-                    P v[8];
+                    P t[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = o[e][s];
-                    __builtin_memcpy(base + s * BO * 128 + place(p >> 3, p & 7), v, 16);
+                    for (int e = 0; e < 8; ++e) t[e] = o[e][s];
+                    __builtin_memcpy(__builtin_assume_aligned(base + s * BO * 128 + place(p >> 3, p & 7), 16), t, 16);
                 }
             }
         }
@@ -171,61 +203,63 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
             __builtin_memcpy(q, &db[i], 16);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                P v[8];
+                P t[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (P)(float)q[h * 8 + e];
-                __builtin_memcpy(base + NP * BO * 128 + place(p >> 2, (p & 3) * 2 + h), v, 16);
+                for (int e = 0; e < 8; ++e) t[e] = (P)(float)q[h * 8 + e];
+                __builtin_memcpy(__builtin_assume_aligned(base + NP * BO * 128 + place(p >> 2, (p & 3) * 2 + h), 16), t, 16);
             }
         }
     };
 
-    f32x16 acc[FO][FC] = {};
-    float unit[FC] = {}, top[FC] = {};             // the scale that the sums are in units of; the largest since they were last put aside
-    bool aside = false;
-    float *const part = a.part + (int64_t)blockIdx.y * a.O * a.C;
-    // sums in full units to `put`; lane l holds channel l % 32 and, in register i, output 8 (i / 4) + 4 (l / 32) + i % 4
-    auto each = [&](auto put) {
+    // the scales of this lane's channels
+    int sat[FC];
 #pragma unroll
-        for (int i = 0; i < FO; ++i)
+    for (int j = 0; j < FC; ++j) sat[j] = min(c0 + (wc * FC + j) * 32 + l32, a.C - 1);
+    float s[FC];
+    auto scales = [&](int blk) {
+        const int b = blk / a.runs;
+        const float *const p = a.scale + (int64_t)b * a.C * a.runs + (blk - b * a.runs);
 #pragma unroll
-            for (int j = 0; j < FC; ++j) {
-                __builtin_amdgcn_sched_barrier(0);          // one accumulator at a time: addresses of all would fill the registers
-                const int c = c0 + (wc * FC + j) * 32 + l32;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int o = o0 + (wo * FO + i) * 32 + 8 * (e / 4) + 4 * half + e % 4;
-                    if (o < a.O && c < a.C) put((int64_t)o * a.C + c, acc[i][j][e] * unit[j]);
-                }
-            }
+        for (int j = 0; j < FC; ++j) s[j] = p[(int64_t)sat[j] * a.runs];
     };
-    const int steps = 2 * (last - first);
-    if (steps > 0) {
-        fetch(0);
+    int blk = first;
+    if (blk < last) {
+        fetch(blk, 0);
+        scales(blk);
         keep(0);
         lds_barrier();
     }
-    for (int k = 0; k < steps; ++k) {
-        if (k + 1 < steps) fetch(k + 1);
-        if ((k & 1) == 0) {
-            const int blk = first + (k >> 1), b = blk / a.runs, j0 = blk - b * a.runs;
-            float s[FC];
-            bool small = false;
+    float *const part = a.part + (int64_t)range * a.O * a.C;
+    // this lane's first pieces of either operand; piece 2 kk + half is at (... ^ kk << 5)
+    const int ro = place(wo * FO * 32 + l32, half), rc = NP * BO * 128 + place(wc * FC * 32 + l32, half);
+    bool aside = false;
+    do {
+        f32x16 acc[FO][FC] = {};
+        float unit[FC] = {}, top[FC] = {};         // the scale that the sums are in units of, and the largest so far
+        auto products = [&](int buf) {
 #pragma unroll
-            for (int j = 0; j < FC; ++j) {
-                const int c = min(c0 + (wc * FC + j) * 32 + l32, a.C - 1);
-                s[j] = a.scale[((int64_t)b * a.C + c) * a.runs + j0];
-                small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
-            }
-            if (__any(small)) {                    // units so much smaller that the sums might leave fp32's range: the sums are put aside
-                each([&](int64_t at, float v) { part[at] = aside ? part[at] + v : v; });
-                aside = true;
+            for (int kk = 0; kk < 4; ++kk) {
+                const char *const pc = lds + buf * STAGE + (rc ^ (kk << 5)), *const po = lds + buf * STAGE + (ro ^ (kk << 5));
+                uint4 fc[FC];
 #pragma unroll
-                for (int j = 0; j < FC; ++j) {
-                    unit[j] = top[j] = 0.f;
+                for (int j = 0; j < FC; ++j) fc[j] = *(const uint4 *)(pc + j * 32 * 128);
 #pragma unroll
-                    for (int i = 0; i < FO; ++i) acc[i][j] = 0.f;
+                for (int p = NP - 1; p >= 0; --p) {        // the smallest parts first
+#pragma unroll
+                    for (int i = 0; i < FO; ++i) {
+                        const uint4 fo = *(const uint4 *)(po + (p * BO + i * 32) * 128);
+#pragma unroll
+                        for (int j = 0; j < FC; ++j) acc[i][j] = mfma16(fo, fc[j], acc[i][j], P());
+                    }
                 }
             }
+        };
+        for (; blk < last; ++blk) {
+            // units so much smaller that the sums might leave fp32's range: the sums so far are put aside
+            bool small = false;
+#pragma unroll
+            for (int j = 0; j < FC; ++j) small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
+            if (__any(small)) break;
 #pragma unroll
             for (int j = 0; j < FC; ++j) {
                 // a run of zeros keeps the units; so do the first sums
@@ -235,30 +269,55 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 #pragma unroll
                 for (int i = 0; i < FO; ++i) acc[i][j] *= f;
             }
-        }
-        const char *const base = lds + (k & 1) * STAGE;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            uint4 fc[FC];
-#pragma unroll
-            for (int j = 0; j < FC; ++j) fc[j] = *(const uint4 *)(base + NP * BO * 128 + place((wc * FC + j) * 32 + l32, kk * 2 + half));
-#pragma unroll
-            for (int p = NP - 1; p >= 0; --p) {    // the smallest parts first
-#pragma unroll
-                for (int i = 0; i < FO; ++i) {
-                    const uint4 fo = *(const uint4 *)(base + p * BO * 128 + place((wo * FO + i) * 32 + l32, kk * 2 + half));
-#pragma unroll
-                    for (int j = 0; j < FC; ++j) acc[i][j] = mfma16(fo, fc[j], acc[i][j], P());
-                }
-            }
-        }
-        if (k + 1 < steps) {
-            keep((k + 1) & 1);
+            const int next = min(blk + 1, last - 1);       // (the last run's own first half once more at the end, not used)
+            fetch(blk, 1);
+            products(0);
+            keep(1);
+            lds_barrier();
+            fetch(next, 0);
+            scales(next);
+            products(1);
+            keep(0);
             lds_barrier();
         }
-    }
-    if (a.splits > 1) each([&](int64_t at, float v) { part[at] = aside ? part[at] + v : v; });
-    else each([&](int64_t at, float v) { ((DW *)a.dw)[at] = from_f32<DW>(aside ? part[at] + v : v); });
+        // lane l holds channel l % 32 and, in register i, output 8 (i / 4) + 4 (l / 32) + i % 4
+        const bool rounded = a.splits == 1 && blk >= last;
+        int o1 = o0 + wo * FO * 32 + 4 * half, c1 = c0 + wc * FC * 32 + l32;
+        asm volatile("" : "+v"(o1), "+v"(c1));                      // (else the compiler keeps all addresses below in registers throughout the sums)
+#pragma unroll
+        for (int i = 0; i < FO; ++i)
+#pragma unroll
+            for (int j = 0; j < FC; ++j) {
+                __builtin_amdgcn_sched_barrier(0);         // one accumulator at a time: addresses of all would fill the registers
+                const int c = c1 + j * 32;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int o = o1 + i * 32 + 8 * (e / 4) + e % 4;
+                    if (o >= a.O || c >= a.C) continue;
+                    const int64_t at = (int64_t)o * a.C + c;
+                    float v = acc[i][j][e] * unit[j];
+                    if (aside) v += part[at];
+                    if (rounded) ((DW *)a.dw)[at] = from_f32<DW>(v);
+                    else part[at] = v;
+                }
+            }
+        aside = true;
+    } while (blk < last);
+}
+
+// Tensors of less than the 16 bytes that a load of the kernel above takes (a handful of values): a thread for each of dw's.
+template <typename T, bool TOKENS, typename DW> __global__ void __launch_bounds__(64) k_weight_tiny(const WeightArgs a)
+{
+    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    if (i >= (int64_t)a.O * a.C) return;
+    const int64_t o = i / a.C, c = i - o * a.C;
+    float sum = 0.f;
+    for (int64_t b = 0; b < a.sequences; ++b)
+        for (int64_t n = 0; n < a.N; ++n) {
+            const float x = (float)a.q[(b * a.C + c) * a.N + n] * a.scale[(b * a.C + c) * a.runs + n / RUN];
+            sum = fmaf(to_f32(((const T *)a.dy)[TOKENS ? (b * a.N + n) * a.O + o : (b * a.O + o) * a.N + n]), x, sum);
+        }
+    ((DW *)a.dw)[i] = from_f32<DW>(sum);
 }
 
 template <typename DW> __global__ void __launch_bounds__(256) k_sum_ranges(const float *__restrict__ part, DW *__restrict__ dw, int splits, int64_t n)
@@ -304,13 +363,19 @@ template <typename T, typename DW> static int run(const WeightShape &w, const We
         constexpr int lds = 2 * (64 * FO * NP + 128 * FC) * 128;
         const auto kernel = k_weight<T, decltype(tok)::value, DW, FO, FC>;
         FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
-        const dim3 grid((unsigned)(((a.O + 64 * FO - 1) / (64 * FO)) * a.tiles_c), (unsigned)a.splits);
-        kernel<<<grid, 512, lds, s>>>(a);
+        kernel<<<(unsigned)(a.tiles * a.splits), 512, lds, s>>>(a);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     };
     using Y = std::true_type;
     using No = std::false_type;
+    if ((int64_t)a.sequences * a.N * a.O * (int64_t)sizeof(T) < 16 || (int64_t)a.sequences * a.N * a.C < 16) {
+        const unsigned g = (unsigned)(((int64_t)a.O * a.C + 63) / 64);
+        if (tokens) k_weight_tiny<T, true, DW><<<g, 64, 0, s>>>(a);
+        else k_weight_tiny<T, false, DW><<<g, 64, 0, s>>>(a);
+        FC_HIP(hipGetLastError());
+        return FFTCONV_OK;
+    }
     if constexpr (sizeof(T) == 2) {
         if (w.fo == 4) {
             const std::integral_constant<int, 4> fo;
@@ -336,9 +401,9 @@ int weight_grad(const void *dy, const int8_t *q, const float *scale, void *dw, i
 {
     const WeightShape w = weight_shape(B, N, O, C, dtype_dy);
     WeightArgs a = {};
-    a.dy = dy, a.q = q, a.scale = scale, a.part = (float *)workspace, a.dw = dw, a.N = N, a.O = (int)O, a.C = (int)C;
+    a.dy = dy, a.q = q, a.scale = scale, a.part = (float *)workspace, a.dw = dw, a.sequences = (int)B, a.N = (int)N, a.O = (int)O, a.C = (int)C;
     a.runs = (int)((N + RUN - 1) / RUN), a.blocks = (int)(B * a.runs), a.per = w.per, a.splits = w.splits;
-    a.tiles_c = (int)((C + 128 * w.fc - 1) / (128 * w.fc));
+    a.tiles_c = (int)((C + 128 * w.fc - 1) / (128 * w.fc)), a.tiles = (int)((O + 64 * w.fo - 1) / (64 * w.fo)) * a.tiles_c;
     auto by_dw = [&](auto t) -> int {
         using T = decltype(t);
         if (dtype_dw == FFTCONV_F32) return run<T, float>(w, a, tokens, s);

@@ -96,6 +96,10 @@ def test_weight_gradient(kw):
     assert weight(**kw) == EINVAL
 
 
+def test_weight_gradient_of_sizes_beyond_its_kernels():
+    assert weight(n=(1 << 22) + 1) == weight(o=1 << 23) == weight(c=1 << 23) == EUNSUPPORTED
+
+
 def test_workspaces_of_what_is_refused_are_empty():
     lib = fftconv.load()
     assert lib.fftconv_workspace_bytes_rms_norm_backward(-1, 64, BF16) == 0
