@@ -86,7 +86,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
     constexpr int STAGE = (BO * NP + BC) * 128;
     extern __shared__ __align__(16) char lds[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
-    const int wo = wave >> 2, wc = wave & 3;
+    const int wo = __builtin_amdgcn_readfirstlane(wave >> 2), wc = wave & 3;
     // workgroups go to the dies in turn; a die takes neighbouring tiles of one range, which read the same dy and q from its L2
     const int n_wg = gridDim.x, die = blockIdx.x % 8, spare = n_wg % 8;
     const int at = die * (n_wg / 8) + min(die, spare) + blockIdx.x / 8;
@@ -227,6 +227,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
         fetch(blk, 0);
         scales(blk);
         keep(0);
+        fetch(blk, 1);
         lds_barrier();
     }
     float *const part = a.part + (int64_t)range * a.O * a.C;
@@ -269,15 +270,17 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 #pragma unroll
                 for (int i = 0; i < FO; ++i) acc[i][j] *= f;
             }
-            const int next = min(blk + 1, last - 1);       // (the last run's own first half once more at the end, not used)
-            fetch(blk, 1);
+            // Each half run: what was asked for a half run ago goes to LDS and the next is asked for, on four waves before the products of the
+            // half run that is there and on four after them, so that on each SIMD one wave's conversions run beside the other's products.
+            const int next = min(blk + 1, last - 1);       // (the last run once more at the end, not used)
+            if (wo == 0) keep(1), fetch(next, 0);
             products(0);
-            keep(1);
+            if (wo != 0) keep(1), fetch(next, 0);
             lds_barrier();
-            fetch(next, 0);
             scales(next);
+            if (wo == 0) keep(0), fetch(next, 1);
             products(1);
-            keep(0);
+            if (wo != 0) keep(0), fetch(next, 1);
             lds_barrier();
         }
         // lane l holds channel l % 32 and, in register i, output 8 (i / 4) + 4 (l / 32) + i % 4
