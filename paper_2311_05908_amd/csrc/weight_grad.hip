@@ -58,6 +58,23 @@ template <typename T, typename P> __device__ __forceinline__ void split(const T 
     }
 }
 
+// Two whole numbers of up to eight bits as a pair of 16-bit ones, exactly: of bf16 the upper halves of the fp32 ones.
+__device__ __forceinline__ uint32_t pair_of(float x, float y, __bf16)
+{
+    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
+}
+__device__ __forceinline__ uint32_t pair_of(float x, float y, _Float16) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y)); }
+template <typename T> __device__ __forceinline__ void widen(uint4 v, uint4 (&o)[2])
+{
+    int8_t q[16];
+    __builtin_memcpy(q, &v, 16);
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = pair_of((float)q[2 * i], (float)q[2 * i + 1], T());
+    o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+
 // 16 bytes from p, of which the first `left` are wanted and the others read as zero, without reading beyond `end` (the tensor's, which has 16
 // bytes at least): what lies too near the end comes from the last 16 bytes, moved down.
 __device__ __forceinline__ uint4 load_edge(const char *p, const char *end, int64_t left)
@@ -77,6 +94,31 @@ template <typename T> __device__ __forceinline__ uint4 load_whole(const T *p, ui
     uint4 r;
     __builtin_memcpy(&r, __builtin_assume_aligned((const char *)p + bytes, alignof(T)), 16);
     return r;
+}
+
+// A wave's sums, in full, to dw (rounded) or to its range's part, on top of those put aside before. Lane l holds channel l % 32 and, in
+// register i, output 8 (i / 4) + 4 (l / 32) + i % 4; o1, c1: this lane's first.
+template <typename DW, int FO, int FC> __device__ __forceinline__ void store_sums(const WeightArgs &a, const f32x16 (&acc)[FO][FC], const float (&unit)[FC],
+                                                                                  float *part, bool aside, bool rounded, int o1, int c1)
+{
+    asm volatile("" : "+v"(o1), "+v"(c1));                 // (else the compiler keeps all addresses below in registers throughout the sums)
+#pragma unroll
+    for (int i = 0; i < FO; ++i)
+#pragma unroll
+        for (int j = 0; j < FC; ++j) {
+            __builtin_amdgcn_sched_barrier(0);             // one accumulator at a time: addresses of all would fill the registers
+            const int c = c1 + j * 32;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int o = o1 + i * 32 + 8 * (e / 4) + e % 4;
+                if (o >= a.O || c >= a.C) continue;
+                const int64_t at = (int64_t)o * a.C + c;
+                float v = acc[i][j][e] * unit[j];
+                if (aside) v += part[at];
+                if (rounded) ((DW *)a.dw)[at] = from_f32<DW>(v);
+                else part[at] = v;
+            }
+        }
 }
 
 template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void __launch_bounds__(512, 2) k_weight(const WeightArgs a)
@@ -199,15 +241,10 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 #pragma unroll
         for (int i = 0; i < BV; ++i) {
             const int p = threadIdx.x + i * 512;
-            int8_t q[16];
-            __builtin_memcpy(q, &db[i], 16);
+            uint4 t[2];
+            widen<P>(db[i], t);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                P t[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) t[e] = (P)(float)q[h * 8 + e];
-                __builtin_memcpy(__builtin_assume_aligned(base + NP * BO * 128 + place(p >> 2, (p & 3) * 2 + h), 16), t, 16);
-            }
+            for (int h = 0; h < 2; ++h) *(uint4 *)(base + NP * BO * 128 + place(p >> 2, (p & 3) * 2 + h)) = t[h];
         }
     };
 
@@ -283,28 +320,196 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
             if (wo != 0) keep(0), fetch(next, 1);
             lds_barrier();
         }
-        // lane l holds channel l % 32 and, in register i, output 8 (i / 4) + 4 (l / 32) + i % 4
-        const bool rounded = a.splits == 1 && blk >= last;
-        int o1 = o0 + wo * FO * 32 + 4 * half, c1 = c0 + wc * FC * 32 + l32;
-        asm volatile("" : "+v"(o1), "+v"(c1));                      // (else the compiler keeps all addresses below in registers throughout the sums)
+        store_sums<DW, FO, FC>(a, acc, unit, part, aside, a.splits == 1 && blk >= last, o0 + wo * FO * 32 + 4 * half, c0 + wc * FC * 32 + l32);
+        aside = true;
+    } while (blk < last);
+}
+
+// The same for 16-bit dy with everything in pieces of 16 bytes (samples a multiple of 16, channels of dy of 8): tiles go from memory straight
+// to LDS, two half runs ahead of the products, as they lie there. dy (b, n, o) is turned over on its way from LDS into the operand: a transposing
+// read gives lane i of sixteen the i-th of 16 channels of four samples, each four lanes having pointed at a sample's 16 channels. q is widened
+// there too.
+//
+// Samples of a half run, as operands want them (8 for a lane of either half of the wave): pair u of products, product v of it, takes
+// 32 u + 16 half + 8 v ..., so that one read of 16 bytes of q serves both.
+__device__ const uint4 zero_piece = {0, 0, 0, 0};
+
+// 16 (or 4) bytes for each lane from base + off to LDS, at `to` + 16 (or 4) * lane: a transfer that no register waits for, counted by vmcnt. Written
+// as instructions because the compiler waits for all such transfers before any read of LDS; FC_ARRIVED below waits for the right ones. (M0, which
+// holds the place in LDS, is used by nothing else in these kernels.)
+__device__ __forceinline__ uint32_t lds_offset(const char *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p; }
+// An address that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const char *uniform(const char *p)
+{
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+    return (const char *)(uintptr_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ void to_lds16(const char *base, uint32_t off, const char *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void to_lds16(const char *from, const char *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(from) : "memory");
+}
+__device__ __forceinline__ void to_lds4(const char *from, const char *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(from) : "memory");
+}
+// Waits until at most `left` of this wave's transfers are on their way, then for the other waves.
+#ifdef FFTCONV_SYNC_CHECK
+#define FC_ARRIVED(left) do { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); __syncthreads(); } while (0)
+#else
+#define FC_ARRIVED(left) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(left) : "memory")
+#endif
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+__device__ __forceinline__ uint2 read_transposed(const char *p)
+{
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
+}
+template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void __launch_bounds__(512, 2) k_weight_async(const WeightArgs a)
+{
+    constexpr int BO = 64 * FO, BC = 128 * FC, Q_AT = BO * 128, S_AT = Q_AT + BC * 64, STAGE = S_AT + 8 * 256, STAGES = 3;
+    extern __shared__ __align__(16) char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+    const int wo = wave >> 2, wc = wave & 3;
+    const int n_wg = gridDim.x, die = blockIdx.x % 8, spare = n_wg % 8;
+    const int at = die * (n_wg / 8) + min(die, spare) + blockIdx.x / 8;
+    const int tile = at % a.tiles, range = at / a.tiles;
+    const int o0 = tile / a.tiles_c * BO, c0 = tile % a.tiles_c * BC;
+    const int first = range * a.per, last = min(first + a.per, a.blocks);
+
+    // What this lane brings to LDS. dy (b, n, o): rows of BO channels of a sample, their 16-byte pieces moved in pairs by the sample, so that the
+    // four samples of a transposing read lie in banks of their own. dy (b, o, n): rows of 64 samples of a channel, pieces moved by the channel.
+    // q: rows of 64 bytes, pieces moved by bits 1-2 of the channel. Channels beyond the end read others: what comes of them is not stored.
+    constexpr int LR = BO / 8;                                   // lanes to a row of (b, n, o)
+    uint32_t aat[FO], bat[FC];
+    int an[FO], bn[FC];                                          // this lane's first sample
 #pragma unroll
-        for (int i = 0; i < FO; ++i)
+    for (int i = 0; i < FO; ++i) {
+        const int p = (wave * FO + i) * 64 + lane;
+        if constexpr (TOKENS) {
+            const int n = p / LR, m = n & 3, piece = (p % LR) ^ (2 * (m ^ (m << 1)));
+            an[i] = n;
+            aat[i] = ((uint32_t)n * (uint32_t)a.O + (o0 + piece * 8 < a.O ? piece * 8 : 0)) * 2;
+        } else {
+            const int o = p >> 3, piece = (p & 7) ^ (o & 7);
+            an[i] = piece * 8;
+            aat[i] = ((uint32_t)(min(o0 + o, a.O - 1) - o0) * (uint32_t)a.N + piece * 8) * 2;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < FC; ++i) {
+        const int p = (wave * FC + i) * 64 + lane, c = p >> 2, piece = (p & 3) ^ ((c >> 1) & 3);
+        bn[i] = piece * 16;
+        bat[i] = (uint32_t)(min(c0 + c, a.C - 1) - c0) * (uint32_t)a.N + piece * 16;
+    }
+    // lane i of a wave's scales is channel i of its 64 (FC = 2) or 32 (FC = 1, twice)
+    const int64_t sat = (int64_t)min(c0 + wc * FC * 32 + (FC == 2 ? lane : l32), a.C - 1) * a.runs;
+
+    auto fetch = [&](int run, int h, int stage) {
+        const int blk = __builtin_amdgcn_readfirstlane(run);     // (the same in all lanes, which the compiler cannot tell)
+        const int b = blk / a.runs, j = blk - b * a.runs, n0 = j * RUN + h * 64;
+        const char *const dy = uniform((const char *)a.dy + (TOKENS ? ((int64_t)b * a.N + n0) * a.O + o0 : ((int64_t)b * a.O + o0) * a.N + n0) * 2);
+        const char *const q = uniform((const char *)a.q + ((int64_t)b * a.C + c0) * a.N + n0);
+        char *const to = lds + stage * STAGE + wave * 1024;
+        if (n0 + 64 <= a.N) {
+#pragma unroll
+            for (int i = 0; i < FO; ++i) to_lds16(dy, aat[i], to + wave * (FO - 1) * 1024 + i * 1024);
+#pragma unroll
+            for (int i = 0; i < FC; ++i) to_lds16(q, bat[i], to + Q_AT + wave * (FC - 1) * 1024 + i * 1024);
+        } else {                                                 // samples beyond the end are zeros
+            const char *const zero = (const char *)&zero_piece;
+#pragma unroll
+            for (int i = 0; i < FO; ++i) to_lds16(n0 + an[i] < a.N ? dy + aat[i] : zero, to + wave * (FO - 1) * 1024 + i * 1024);
+#pragma unroll
+            for (int i = 0; i < FC; ++i) to_lds16(n0 + bn[i] < a.N ? q + bat[i] : zero, to + Q_AT + wave * (FC - 1) * 1024 + i * 1024);
+        }
+        if (h == 0) to_lds4((const char *)(a.scale + (int64_t)b * a.C * a.runs + j + sat), lds + stage * STAGE + S_AT + wave * 256);
+    };
+    // where this lane reads its operands, from a stage's start
+    int ra[TOKENS ? FO : 1];
+    if constexpr (TOKENS) {
+        const int j = lane & 15, m = j >> 2;
+#pragma unroll
+        for (int i = 0; i < FO; ++i) {
+            const int piece = ((wo * FO + i) * 4 + 2 * ((lane >> 4) & 1) + ((j & 3) >> 1)) ^ (2 * (m ^ (m << 1)));
+            ra[i] = (16 * half + m) * BO * 2 + piece * 16 + (j & 1) * 8;
+        }
+    } else {
+        ra[0] = (wo * FO * 32 + l32) * 128 + (((2 * half) ^ (l32 & 7)) << 4);
+    }
+    const int rq = Q_AT + (wc * FC * 32 + l32) * 64 + ((half ^ ((l32 >> 1) & 3)) << 4);
+
+    float *const part = a.part + (int64_t)range * a.O * a.C;
+    bool aside = false;
+    int blk = first, stage = 0;
+    if (blk < last) {
+        fetch(blk, 0, 0);
+        fetch(blk, 1, 1);
+        FC_ARRIVED(FO + FC);
+    }
+    do {
+        f32x16 acc[FO][FC] = {};
+        float unit[FC] = {}, top[FC] = {};
+        auto products = [&](const char *base) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint4 fc[FC][2];
+#pragma unroll
+                for (int j = 0; j < FC; ++j) widen<T>(*(const uint4 *)(base + (rq ^ (u << 5)) + j * 32 * 64), fc[j]);
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+#pragma unroll
+                    for (int i = 0; i < FO; ++i) {
+                        uint4 fo;
+                        if constexpr (TOKENS) {
+                            const char *const p = base + ra[i] + (32 * u + 8 * v) * BO * 2;
+                            const uint2 x = read_transposed(p), y = read_transposed(p + 4 * BO * 2);
+                            fo = make_uint4(x.x, x.y, y.x, y.y);
+                        } else {
+                            fo = *(const uint4 *)(base + (ra[0] ^ (u << 6 | v << 4)) + i * 32 * 128);
+                        }
+#pragma unroll
+                        for (int j = 0; j < FC; ++j) acc[i][j] = mfma16(fo, fc[j][v], acc[i][j], T());
+                    }
+            }
+        };
+        for (; blk < last; ++blk) {
+            // the first half is there; so is the second, or on its way
+            const char *base = lds + stage * STAGE;
+            float s[FC];
+            bool small = false;
 #pragma unroll
             for (int j = 0; j < FC; ++j) {
-                __builtin_amdgcn_sched_barrier(0);         // one accumulator at a time: addresses of all would fill the registers
-                const int c = c1 + j * 32;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int o = o1 + i * 32 + 8 * (e / 4) + e % 4;
-                    if (o >= a.O || c >= a.C) continue;
-                    const int64_t at = (int64_t)o * a.C + c;
-                    float v = acc[i][j][e] * unit[j];
-                    if (aside) v += part[at];
-                    if (rounded) ((DW *)a.dw)[at] = from_f32<DW>(v);
-                    else part[at] = v;
-                }
+                s[j] = *(const float *)(base + S_AT + wave * 256 + (j * 32 + l32) * 4);
+                small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
             }
+            if (__any(small)) break;
+            const int next = min(blk + 1, last - 1);             // (the last run once more at the end, not used)
+            int free = stage + 2 < STAGES ? stage + 2 : stage + 2 - STAGES;
+            fetch(next, 0, free);
+#pragma unroll
+            for (int j = 0; j < FC; ++j) {
+                const float f = s[j] == 0.f || unit[j] == 0.f ? 1.f : unit[j] / s[j];
+                unit[j] = s[j] == 0.f ? unit[j] : s[j];
+                top[j] = fmaxf(top[j], unit[j]);
+#pragma unroll
+                for (int i = 0; i < FO; ++i) acc[i][j] *= f;
+            }
+            products(base);
+            FC_ARRIVED(FO + FC + 1);
+            free = stage, stage = stage + 1 < STAGES ? stage + 1 : 0;
+            fetch(next, 1, free);
+            products(lds + stage * STAGE);
+            FC_ARRIVED(FO + FC);
+            stage = stage + 1 < STAGES ? stage + 1 : 0;
+        }
+        store_sums<DW, FO, FC>(a, acc, unit, part, aside, a.splits == 1 && blk >= last, o0 + wo * FO * 32 + 4 * half, c0 + wc * FC * 32 + l32);
         aside = true;
+        // stores count as the transfers do; and nothing is on its way to LDS when the workgroup ends
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     } while (blk < last);
 }
 
@@ -363,6 +568,17 @@ template <typename T, typename DW> static int run(const WeightShape &w, const We
 {
     auto launch = [&](auto tok, auto fo, auto fc) -> int {
         constexpr int FO = decltype(fo)::value, FC = decltype(fc)::value, NP = Operand<T>::PARTS;
+        if constexpr (NP == 1) {
+            const bool pieces = a.N % 16 == 0 && (!tokens || a.O % 8 == 0) && ((uintptr_t)a.dy | (uintptr_t)a.q) % 16 == 0;
+            if (pieces) {
+                constexpr int lds = 3 * (64 * FO * 128 + 128 * FC * 64 + 8 * 256);
+                const auto kernel = k_weight_async<T, decltype(tok)::value, DW, FO, FC>;
+                FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
+                kernel<<<(unsigned)(a.tiles * a.splits), 512, lds, s>>>(a);
+                FC_HIP(hipGetLastError());
+                return FFTCONV_OK;
+            }
+        }
         constexpr int lds = 2 * (64 * FO * NP + 128 * FC) * 128;
         const auto kernel = k_weight<T, decltype(tok)::value, DW, FO, FC>;
         FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
