@@ -297,7 +297,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
             bool small = false;
 #pragma unroll
             for (int j = 0; j < FC; ++j) small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
-            if (__any(small)) break;
+            if (__builtin_amdgcn_ballot_w64(small) != 0) break;
 #pragma unroll
             for (int j = 0; j < FC; ++j) {
                 // a run of zeros keeps the units; so do the first sums
@@ -326,7 +326,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 }
 
 // The same for 16-bit dy with everything in pieces of 16 bytes (samples a multiple of 16, channels of dy of 8): tiles go from memory straight
-// to LDS, two half runs ahead of the products, as they lie there. dy (b, n, o) is turned over on its way from LDS into the operand: a transposing
+// to LDS, three half runs ahead of the products, as they lie there. dy (b, n, o) is turned over on its way from LDS into the operand: a transposing
 // read gives lane i of sixteen the i-th of 16 channels of four samples, each four lanes having pointed at a sample's 16 channels. q is widened
 // there too.
 //
@@ -353,9 +353,9 @@ __device__ __forceinline__ void to_lds16(const char *from, const char *to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(from) : "memory");
 }
-__device__ __forceinline__ void to_lds4(const char *from, const char *to)
+__device__ __forceinline__ void to_lds4(const char *base, uint32_t off, const char *to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(off), "s"(base) : "memory");
 }
 // Waits until at most `left` of this wave's transfers are on their way, then for the other waves.
 #ifdef FFTCONV_SYNC_CHECK
@@ -406,28 +406,47 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
         bat[i] = (uint32_t)(min(c0 + c, a.C - 1) - c0) * (uint32_t)a.N + piece * 16;
     }
     // lane i of a wave's scales is channel i of its 64 (FC = 2) or 32 (FC = 1, twice)
-    const int64_t sat = (int64_t)min(c0 + wc * FC * 32 + (FC == 2 ? lane : l32), a.C - 1) * a.runs;
+    const uint32_t sat = (uint32_t)(min(c0 + wc * FC * 32 + (FC == 2 ? lane : l32), a.C - 1) - c0) * (uint32_t)a.runs * 4;
 
-    auto fetch = [&](int run, int h, int stage) {
-        const int blk = __builtin_amdgcn_readfirstlane(run);     // (the same in all lanes, which the compiler cannot tell)
-        const int b = blk / a.runs, j = blk - b * a.runs, n0 = j * RUN + h * 64;
-        const char *const dy = uniform((const char *)a.dy + (TOKENS ? ((int64_t)b * a.N + n0) * a.O + o0 : ((int64_t)b * a.O + o0) * a.N + n0) * 2);
-        const char *const q = uniform((const char *)a.q + ((int64_t)b * a.C + c0) * a.N + n0);
-        char *const to = lds + stage * STAGE + wave * 1024;
-        if (n0 + 64 <= a.N) {
+    // What is asked for next: the half run from sample `at_n` of sequence `at_b` on (kept, not divided out of the run's number each time).
+    const int b0 = first / a.runs;
+    int at_b = b0, at_n = (first - b0 * a.runs) * RUN, left = 2 * (last - first);
+    const int64_t dy_step = TOKENS ? (int64_t)a.O * 128 : 128;
+    const char *dy, *q, *sc;
+    auto from_start = [&] {
+        dy = ((const char *)a.dy + (TOKENS ? ((int64_t)at_b * a.N + at_n) * a.O + o0 : ((int64_t)at_b * a.O + o0) * a.N + at_n) * 2);
+        q = ((const char *)a.q + ((int64_t)at_b * a.C + c0) * a.N + at_n);
+        sc = ((const char *)(a.scale + ((int64_t)at_b * a.C + c0) * a.runs + at_n / RUN));
+    };
+    from_start();
+    // (beyond the range's end its last half run once more, not used)
+    auto fetch = [&](int h, int stage) {
+        const char *const to = lds + stage * STAGE;
+        // (the same in all lanes, which the compiler cannot tell)
+        dy = uniform(dy), q = uniform(q), sc = uniform(sc);
+        if (at_n + 64 <= a.N) {
 #pragma unroll
-            for (int i = 0; i < FO; ++i) to_lds16(dy, aat[i], to + wave * (FO - 1) * 1024 + i * 1024);
+            for (int i = 0; i < FO; ++i) to_lds16(dy, aat[i], to + (wave * FO + i) * 1024);
 #pragma unroll
-            for (int i = 0; i < FC; ++i) to_lds16(q, bat[i], to + Q_AT + wave * (FC - 1) * 1024 + i * 1024);
+            for (int i = 0; i < FC; ++i) to_lds16(q, bat[i], to + Q_AT + (wave * FC + i) * 1024);
         } else {                                                 // samples beyond the end are zeros
             const char *const zero = (const char *)&zero_piece;
 #pragma unroll
-            for (int i = 0; i < FO; ++i) to_lds16(n0 + an[i] < a.N ? dy + aat[i] : zero, to + wave * (FO - 1) * 1024 + i * 1024);
+            for (int i = 0; i < FO; ++i) to_lds16(at_n + an[i] < a.N ? dy + aat[i] : zero, to + (wave * FO + i) * 1024);
 #pragma unroll
-            for (int i = 0; i < FC; ++i) to_lds16(n0 + bn[i] < a.N ? q + bat[i] : zero, to + Q_AT + wave * (FC - 1) * 1024 + i * 1024);
+            for (int i = 0; i < FC; ++i) to_lds16(at_n + bn[i] < a.N ? q + bat[i] : zero, to + Q_AT + (wave * FC + i) * 1024);
         }
-        if (h == 0) to_lds4((const char *)(a.scale + (int64_t)b * a.C * a.runs + j + sat), lds + stage * STAGE + S_AT + wave * 256);
+        if (h == 0) to_lds4(sc, sat, to + S_AT + wave * 256);
+        if (--left <= 0) return;
+        if (h == 0 || at_n + 64 < a.N) {
+            at_n += 64, dy += dy_step, q += 64;
+            if (h) sc += 4;
+        } else {
+            at_n = 0, ++at_b;
+            from_start();
+        }
     };
+
     // where this lane reads its operands, from a stage's start
     int ra[TOKENS ? FO : 1];
     if constexpr (TOKENS) {
@@ -442,54 +461,93 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
     }
     const int rq = Q_AT + (wc * FC * 32 + l32) * 64 + ((half ^ ((l32 >> 1) & 3)) << 4);
 
+    // The operands of the products of a half run, in four groups 2 u + v: of dy one group ahead of its products, of q a pair of groups.
+    uint4 fo[2][FO], fc[2][FC][2], raw[FC];
+    auto read_dy = [&](const char *base, int g) {
+        const int u = g >> 1, v = g & 1;
+#pragma unroll
+        for (int i = 0; i < FO; ++i) {
+            if constexpr (TOKENS) {
+                const char *const p = base + ra[i] + (32 * u + 8 * v) * BO * 2;
+                const uint2 x = read_transposed(p), y = read_transposed(p + 4 * BO * 2);
+                fo[g & 1][i] = make_uint4(x.x, x.y, y.x, y.y);
+            } else {
+                fo[g & 1][i] = *(const uint4 *)(base + (ra[0] ^ (u << 6 | v << 4)) + i * 32 * 128);
+            }
+        }
+    };
+    auto read_q = [&](const char *base, int u) {
+#pragma unroll
+        for (int j = 0; j < FC; ++j) raw[j] = *(const uint4 *)(base + (rq ^ (u << 5)) + j * 32 * 64);
+    };
+    auto widen_q = [&](int u) {
+#pragma unroll
+        for (int j = 0; j < FC; ++j) widen<T>(raw[j], fc[u][j]);
+    };
     float *const part = a.part + (int64_t)range * a.O * a.C;
     bool aside = false;
     int blk = first, stage = 0;
+    float s[FC] = {};
+    auto read_scales = [&](const char *base) {
+#pragma unroll
+        for (int j = 0; j < FC; ++j) s[j] = *(const float *)(base + S_AT + wave * 256 + (j * 32 + l32) * 4);
+    };
     if (blk < last) {
-        fetch(blk, 0, 0);
-        fetch(blk, 1, 1);
-        FC_ARRIVED(FO + FC);
+        fetch(0, 0);
+        fetch(1, 1);
+        fetch(0, 2);
+        FC_ARRIVED(2 * (FO + FC) + 1);
+        read_scales(lds);
+        read_dy(lds, 0);
+        read_q(lds, 0);
+        widen_q(0);
     }
     do {
         f32x16 acc[FO][FC] = {};
         float unit[FC] = {}, top[FC] = {};
-        auto products = [&](const char *base) {
+        auto products = [&](int g) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint4 fc[FC][2];
+            for (int i = 0; i < FO; ++i)
 #pragma unroll
-                for (int j = 0; j < FC; ++j) widen<T>(*(const uint4 *)(base + (rq ^ (u << 5)) + j * 32 * 64), fc[j]);
-#pragma unroll
-                for (int v = 0; v < 2; ++v)
-#pragma unroll
-                    for (int i = 0; i < FO; ++i) {
-                        uint4 fo;
-                        if constexpr (TOKENS) {
-                            const char *const p = base + ra[i] + (32 * u + 8 * v) * BO * 2;
-                            const uint2 x = read_transposed(p), y = read_transposed(p + 4 * BO * 2);
-                            fo = make_uint4(x.x, x.y, y.x, y.y);
-                        } else {
-                            fo = *(const uint4 *)(base + (ra[0] ^ (u << 6 | v << 4)) + i * 32 * 128);
-                        }
-#pragma unroll
-                        for (int j = 0; j < FC; ++j) acc[i][j] = mfma16(fo, fc[j][v], acc[i][j], T());
-                    }
-            }
+                for (int j = 0; j < FC; ++j) acc[i][j] = mfma16(fo[g & 1][i], fc[g >> 1][j][g & 1], acc[i][j], T());
+        };
+        // The products of the half run at `stage`. Before the last group every wave has read all of it, and the next half run has arrived: beside that
+        // group the next one's first operands are read, and what comes three half runs later is asked for, to the same place.
+        auto half_run = [&](auto second) {
+            constexpr int H = decltype(second)::value;
+            const char *const base = lds + stage * STAGE;
+            read_dy(base, 1);
+            read_q(base, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            products(0);
+            __builtin_amdgcn_sched_barrier(0);
+            read_dy(base, 2);
+            __builtin_amdgcn_sched_barrier(0);
+            widen_q(1);
+            products(1);
+            __builtin_amdgcn_sched_barrier(0);
+            read_dy(base, 3);
+            __builtin_amdgcn_sched_barrier(0);
+            products(2);
+            __builtin_amdgcn_sched_barrier(0);
+            FC_ARRIVED(FO + FC + (H ? 0 : 1));                   // on its way may be the half run after the next
+            const int free = stage;
+            stage = stage + 1 < STAGES ? stage + 1 : 0;
+            const char *const next = lds + stage * STAGE;
+            if constexpr (H) read_scales(next);
+            read_dy(next, 0);
+            read_q(next, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(1 - H, free);
+            widen_q(0);
+            products(3);
+            __builtin_amdgcn_sched_barrier(0);
         };
         for (; blk < last; ++blk) {
-            // the first half is there; so is the second, or on its way
-            const char *base = lds + stage * STAGE;
-            float s[FC];
             bool small = false;
 #pragma unroll
-            for (int j = 0; j < FC; ++j) {
-                s[j] = *(const float *)(base + S_AT + wave * 256 + (j * 32 + l32) * 4);
-                small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
-            }
-            if (__any(small)) break;
-            const int next = min(blk + 1, last - 1);             // (the last run once more at the end, not used)
-            int free = stage + 2 < STAGES ? stage + 2 : stage + 2 - STAGES;
-            fetch(next, 0, free);
+            for (int j = 0; j < FC; ++j) small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
+            if (__builtin_amdgcn_ballot_w64(small) != 0) break;
 #pragma unroll
             for (int j = 0; j < FC; ++j) {
                 const float f = s[j] == 0.f || unit[j] == 0.f ? 1.f : unit[j] / s[j];
@@ -498,13 +556,8 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 #pragma unroll
                 for (int i = 0; i < FO; ++i) acc[i][j] *= f;
             }
-            products(base);
-            FC_ARRIVED(FO + FC + 1);
-            free = stage, stage = stage + 1 < STAGES ? stage + 1 : 0;
-            fetch(next, 1, free);
-            products(lds + stage * STAGE);
-            FC_ARRIVED(FO + FC);
-            stage = stage + 1 < STAGES ? stage + 1 : 0;
+            half_run(std::integral_constant<int, 0>());
+            half_run(std::integral_constant<int, 1>());
         }
         store_sums<DW, FO, FC>(a, acc, unit, part, aside, a.splits == 1 && blk >= last, o0 + wo * FO * 32 + 4 * half, c0 + wc * FC * 32 + l32);
         aside = true;
