@@ -5,7 +5,7 @@
 // One kernel serves both layouts of y. Its two operands, both with k contiguous, are R, whose rows lie next to each other in y, and S:
 // token by token (t, o) R is the weight, channel by channel (parts, b, o / parts, n) R is the tokens. An accumulator of the matrix cores holds
 // four consecutive rows of R for one row of S in a lane, so the values that a lane stores are neighbours in y either way.
-#include "layers_internal.h"
+#include "async_lds.h"
 
 namespace fftconv {
 namespace lay {
@@ -118,6 +118,37 @@ template <typename T> __device__ __forceinline__ void epilogue(const LinArgs &a,
     }
 }
 
+// The same inside y, with runs of rows that are neighbours in y: no conditions, and 16 bytes to each store. at[]: the places of this lane's runs of
+// rows (8 values of 16 bits: rows 8 half and 16 + 8 half; 4 of fp32: rows 8 j + 4 half).
+template <typename T> __device__ __forceinline__ void epilogue_whole(T *y, const i32x16 &acc, const f32x4 (&rs)[4], const f32x4 (&rb)[4], float ss, float sb,
+                                                                     const int64_t (&at)[sizeof(T)])
+{
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = fmaf((float)acc[i] * rs[i / 4][i % 4], ss, rb[i / 4][i % 4] + sb);
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) __builtin_memcpy(y + at[j], v + 4 * j, 16);
+    } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const T p[2] = {from_f32<T>(v[2 * i]), from_f32<T>(v[2 * i + 1])};
+            __builtin_memcpy(&w[i], p, 4);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const auto x = __builtin_amdgcn_permlane32_swap(w[2 * j + i], w[2 * j + 2 + i], false, false);
+                o[i] = x[0], o[i + 2] = x[1];
+            }
+            __builtin_memcpy(y + at[j / 2], o, 16);
+        }
+    }
+}
+
 template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) k_linear(const LinArgs a)
 {
     using G = Tile<FR, FS>;
@@ -188,6 +219,179 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) 
             epilogue<T>(a, acc[i][j], rbase, s, rs, rb, a.sscale[sc], a.sbias ? a.sbias[sc] : 0.f, column_of(a, sc));
         }
     }
+}
+
+// The same for operands in pieces of 16 bytes (K a multiple of 16): 2 x 4 waves, pieces straight to LDS three steps of 64 ahead of the products,
+// operands in registers one group ahead. A workgroup takes one tile after the other without a pause in the stream of pieces: what is asked for
+// during a tile's last steps is the next tile's, so neither its first loads nor the stores of the one before are waited for.
+//
+// Which tile: workgroups go to the dies in turn; a die takes a stretch of the tiles, its workgroups side by side, in an order in which
+// neighbours share rows of R or of S, so that those come from its L2.
+struct Walk {
+    int tiles_s, group, tiles;
+    __device__ __forceinline__ void place(int i, int &tr, int &ts, int tiles_r) const
+    {
+        const int whole = tiles_r * group, g = i / whole, k = i - g * whole, width = min(group, tiles_s - g * group);
+        tr = k / width, ts = g * group + (k - tr * width);
+    }
+};
+
+template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) k_linear_async(const LinArgs a, const Walk walk)
+{
+    constexpr int BR = 64 * FR, BS = 128 * FS, BK = 64, STAGE = (BR + BS) * BK, STAGES = 4, LI = (BR + BS) / 128;
+    static_assert(BR == BS, "waves 0-3 bring R, 4-7 bring S");
+    extern __shared__ __align__(16) char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+    const int wr = wave >> 2, wsv = wave & 3;
+    // tiles first, first + stride, ... below last
+    const int wgs = gridDim.x, die = blockIdx.x % 8, dies = min(8, wgs), on_die = (wgs - die + 7) / 8;
+    const int begin = (int)((int64_t)walk.tiles * die / dies), last = (int)((int64_t)walk.tiles * (die + 1) / dies);
+    const int first = begin + blockIdx.x / 8;
+    const int steps = (int)((a.K + BK - 1) / BK);
+    const bool tail = a.K % BK != 0;
+
+    // This wave brings rows 16 LI w' ... of R (waves 0-3) or S (4-7), sixteen with an instruction, a piece of 16 bytes for each lane, moved as
+    // piece_at has it.
+    const bool is_r = wave < 4;
+    const int8_t *const src = is_r ? a.r : a.s;
+    const int rows = is_r ? a.nr : a.ns, block = is_r ? BR : BS;
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * LI * 1024;
+    int f_tile = first, f_step = 0;                              // what is asked for next
+    const char *base = nullptr;
+    uint32_t off[LI];
+    auto aim = [&] {                                             // at tile f_tile, or, after the last, once more at it
+        int tr, ts;
+        walk.place(min(f_tile, last - 1), tr, ts, a.tiles_r);
+        const int row0 = (is_r ? tr : ts) * block;
+        base = (const char *)src + (int64_t)row0 * a.K - 3072;
+#pragma unroll
+        for (int i = 0; i < LI; ++i) {
+            const int row = (wave & 3) * 16 * LI + i * 16 + (lane >> 2), piece = (lane & 3) ^ ((row >> 1) & 3);
+            off[i] = (uint32_t)(min(row0 + row, rows - 1) - row0) * (uint32_t)a.K + piece * 16 + 3072 - i * 1024;
+        }
+    };
+    auto fetch = [&](int stage) {
+        if (tail && f_step == steps - 1) {                       // what lies beyond K reads as zeros
+#pragma unroll
+            for (int i = 0; i < LI; ++i) {
+                const int piece = (lane & 3) ^ ((lane >> 3) & 3);
+                const char *const from = base + off[i] + i * 1024;
+                to_lds16((int64_t)f_step * BK + piece * 16 < a.K ? from : (const char *)&zero_piece, lds + stage * STAGE + (wave * LI + i) * 1024);
+            }
+        } else {
+            to_lds16_rows<LI>(uniform(base), off, __builtin_amdgcn_readfirstlane(to + stage * STAGE));
+        }
+        base += BK;
+        if (++f_step == steps) {
+            f_step = 0, f_tile += on_die;
+            aim();
+        }
+    };
+
+    if (first >= last) return;
+    aim();
+    fetch(0);
+    fetch(1);
+    fetch(2);
+    // where this lane's pieces are, from a stage's start: of k 0 ... 31, and of k 32 ... 63 at ^ 32
+    const int ro = piece_at(wr * FR * 32 + l32, half), so = BR * 64 + piece_at(wsv * FS * 32 + l32, half);
+    uint4 fr[2][FR], fs[2][FS];
+    auto read = [&](const char *stage, int kk) {
+#pragma unroll
+        for (int i = 0; i < FR; ++i) fr[kk][i] = *(const uint4 *)(stage + (ro ^ (kk << 5)) + i * 2048);
+#pragma unroll
+        for (int j = 0; j < FS; ++j) fs[kk][j] = *(const uint4 *)(stage + (so ^ (kk << 5)) + j * 2048);
+    };
+    // Scales and biases of this wave's rows of a tile come to LDS at the tile's beginning, to a place of the wave's own, two tiles in turn.
+    constexpr int NR = FR / 2, PRIVATE = (2 * NR + 2) * 256, SCALES = 2 * NR + 2;
+    const char *const own = lds + STAGES * STAGE + wave * 2 * PRIVATE;
+    int tr, ts, parity = 0;
+    auto fetch_scales = [&] {
+        const char *const at = own + parity * PRIVATE;
+        const int r = tr * BR + wr * FR * 32 + lane, sc = min(ts * BS + wsv * FS * 32 + (FS == 2 ? lane : l32), a.ns - 1);
+        const char *const zero = (const char *)&zero_piece;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const uint32_t o = (uint32_t)min(r + i * 64, a.nr - 1) * 4u;
+            to_lds4(uniform((const char *)a.rscale), o, at + i * 256);
+            to_lds4(uniform(a.rbias ? (const char *)a.rbias : zero), a.rbias ? o : 0, at + (NR + i) * 256);
+        }
+        to_lds4(uniform((const char *)a.sscale), (uint32_t)sc * 4u, at + 2 * NR * 256);
+        to_lds4(uniform(a.sbias ? (const char *)a.sbias : zero), a.sbias ? (uint32_t)sc * 4u : 0, at + (2 * NR + 1) * 256);
+    };
+    constexpr int STORES = FR * FS * (sizeof(T) == 4 ? 4 : 2);   // of a whole tile, at least
+    FC_ARRIVED(2 * LI);
+    read(lds, 0);
+    int stage = 0, young = 0;                                    // steps at whose barrier the last tile's stores may still be on their way
+    for (int tile = first; tile < last; tile += on_die) {
+        walk.place(tile, tr, ts, a.tiles_r);
+        fetch_scales();
+        i32x16 acc[FR][FS] = {};
+        auto products = [&](int kk) {
+#pragma unroll
+            for (int i = 0; i < FR; ++i)
+#pragma unroll
+                for (int j = 0; j < FS; ++j) acc[i][j] = mfma_i8(fr[kk][i], fs[kk][j], acc[i][j]);
+        };
+        for (int k = 0; k < steps; ++k) {
+            const char *const here = lds + stage * STAGE;
+            fetch(stage == 0 ? STAGES - 1 : stage - 1);          // (every wave had read that stage before the last barrier)
+            read(here, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            products(0);
+            __builtin_amdgcn_sched_barrier(0);
+            // The next step's pieces are there; those of the two after it may be on their way, and at a tile's first two steps the stores of the tile
+            // before it and its scales, which were sent off after the pieces that are waited for.
+            if (young) {
+                FC_ARRIVED(2 * LI + STORES + SCALES);
+                --young;
+            } else {
+                FC_ARRIVED(2 * LI);
+            }
+            stage = stage + 1 < STAGES ? stage + 1 : 0;
+            read(lds + stage * STAGE, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            products(1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // (three steps after they were asked for the scales are there; with fewer steps they are waited for)
+        if (steps < 3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const char *const sc = own + parity * PRIVATE;
+        parity ^= 1;
+        const int r0 = tr * BR, s0 = ts * BS;
+        constexpr int W = 16 / sizeof(T);
+        const bool whole = r0 + BR <= a.nr && s0 + BS <= a.ns && (!a.channels || a.N % W == 0);
+        young = whole ? 2 : 0;
+#pragma unroll
+        for (int i = 0; i < FR; ++i) {
+            const int rbase = r0 + (wr * FR + i) * 32;
+            f32x4 rs[4], rb[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                rs[q] = *(const f32x4 *)(sc + (i * 32 + 8 * q + 4 * half) * 4);
+                rb[q] = *(const f32x4 *)(sc + (NR * 64 + i * 32 + 8 * q + 4 * half) * 4);
+            }
+            int64_t at[sizeof(T)];
+            if (whole) {
+#pragma unroll
+                for (int q = 0; q < (int)sizeof(T); ++q) at[q] = row_of(a, rbase + (sizeof(T) == 4 ? 8 * q + 4 * half : 16 * q + 8 * half));
+            }
+#pragma unroll
+            for (int j = 0; j < FS; ++j) {
+                const int s = s0 + (wsv * FS + j) * 32 + l32;
+                const float ss = *(const float *)(sc + (2 * NR * 64 + j * 32 + l32) * 4), sb = *(const float *)(sc + ((2 * NR + 1) * 64 + j * 32 + l32) * 4);
+                if (whole) {
+                    epilogue_whole<T>((T *)a.y + column_of(a, s), acc[i][j], rs, rb, ss, sb, at);
+                } else {
+                    float rsv[16], rbv[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) rsv[e] = rs[e / 4][e % 4], rbv[e] = rb[e / 4][e % 4];
+                    epilogue<T>(a, acc[i][j], rbase, s, rsv, rbv, ss, sb, column_of(a, min(s, a.ns - 1)));
+                }
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // nothing is on its way to LDS when the workgroup ends
 }
 
 // Few tokens (S, up to 16 NT of them): what counts is how fast the weight streams in, so its rows go from memory straight into the
@@ -275,7 +479,21 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     };
+    auto launch_async = [&](auto fr, auto fs) -> int {
+        constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value, BR = 64 * FR, BS = 128 * FS, lds = 4 * (BR + BS) * 64 + 16 * (FR + 2) * 256;
+        a.tiles_r = (a.nr + BR - 1) / BR, a.tiles_s = (a.ns + BS - 1) / BS;
+        Walk w = {a.tiles_s, a.tiles_s <= 12 ? a.tiles_s : 8, a.tiles_r * a.tiles_s};
+        const auto kernel = k_linear_async<T, FR, FS>;
+        FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
+        const int most = 256 * (FR == 4 ? 1 : 2);
+        kernel<<<(unsigned)(w.tiles < most ? w.tiles : most), 512, lds, s>>>(a, w);
+        FC_HIP(hipGetLastError());
+        return FFTCONV_OK;
+    };
     auto tiles = [&](int br, int bs) { return (int64_t)((a.nr + br - 1) / br) * ((a.ns + bs - 1) / bs); };
+    const bool pieces = K % 16 == 0 && ((uintptr_t)xq | (uintptr_t)wq) % 16 == 0;
+    if (pieces && tiles(256, 256) >= 256) return launch_async(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+    if (pieces && tiles(128, 128) >= 128) return launch_async(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
     if (tiles(128, 256) >= 512) return launch(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
     if (tiles(128, 128) >= 256) return launch(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
     return launch(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());

@@ -8,7 +8,7 @@
 // the old scale and the new one from run to run, in fp32.
 //
 // A workgroup takes a tile of dw and a range of runs; the ranges' sums are added up in their order by a second kernel.
-#include "layers_internal.h"
+#include "async_lds.h"
 
 namespace fftconv {
 namespace lay {
@@ -332,37 +332,6 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 //
 // Samples of a half run, as operands want them (8 for a lane of either half of the wave): pair u of products, product v of it, takes
 // 32 u + 16 half + 8 v ..., so that one read of 16 bytes of q serves both.
-__device__ const uint4 zero_piece = {0, 0, 0, 0};
-
-// 16 (or 4) bytes for each lane from base + off to LDS, at `to` + 16 (or 4) * lane: a transfer that no register waits for, counted by vmcnt. Written
-// as instructions because the compiler waits for all such transfers before any read of LDS; FC_ARRIVED below waits for the right ones. (M0, which
-// holds the place in LDS, is used by nothing else in these kernels.)
-__device__ __forceinline__ uint32_t lds_offset(const char *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p; }
-// An address that is the same in all lanes, in scalar registers.
-__device__ __forceinline__ const char *uniform(const char *p)
-{
-    const uint64_t v = (uint64_t)(uintptr_t)p;
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
-    return (const char *)(uintptr_t)((uint64_t)hi << 32 | lo);
-}
-__device__ __forceinline__ void to_lds16(const char *base, uint32_t off, const char *to)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(off), "s"(base) : "memory");
-}
-__device__ __forceinline__ void to_lds16(const char *from, const char *to)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(from) : "memory");
-}
-__device__ __forceinline__ void to_lds4(const char *base, uint32_t off, const char *to)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(off), "s"(base) : "memory");
-}
-// Waits until at most `left` of this wave's transfers are on their way, then for the other waves.
-#ifdef FFTCONV_SYNC_CHECK
-#define FC_ARRIVED(left) do { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); __syncthreads(); } while (0)
-#else
-#define FC_ARRIVED(left) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(left) : "memory")
-#endif
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 __device__ __forceinline__ uint2 read_transposed(const char *p)
 {
