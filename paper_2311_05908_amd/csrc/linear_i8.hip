@@ -18,23 +18,32 @@ struct LinArgs {
     int nr, ns;
     int channels;                 // y channel by channel: R is b * N + n, S is o
     int N, per_part;              // samples of a sequence; output channels of a part
+    uint32_t by_n, by_part;       // 2^32 over these, rounded up
     int64_t B;
     int tiles_r, tiles_s;
 };
+
+// x / d for 0 <= x < 2^31 from the reciprocal: at most one too large before the correction.
+__device__ __forceinline__ int quotient(int x, int d, uint32_t by_d)
+{
+    if (d == 1) return x;
+    const uint32_t q = __umulhi((uint32_t)x, by_d);
+    return (int)(q - (q * (uint32_t)d > (uint32_t)x ? 1 : 0));
+}
+static uint32_t reciprocal(int64_t d) { return d > 1 ? (uint32_t)((((int64_t)1 << 32) + d - 1) / d) : 0; }
 
 // First value of y in row s of S: y[column(s) + offset(r)].
 __device__ __forceinline__ int64_t column_of(const LinArgs &a, int s)
 {
     if (!a.channels) return (int64_t)s * a.nr;
-    const int part = s / a.per_part;
-    return ((int64_t)part * a.B * a.per_part + (s - part * a.per_part)) * a.N;
+    return (s + quotient(s, a.per_part, a.by_part) * (a.B - 1) * a.per_part) * a.N;
 }
 // ... and the place of row r of R in it.
 __device__ __forceinline__ int64_t row_of(const LinArgs &a, int r)
 {
     if (!a.channels) return r;
-    const int b = r / a.N;
-    return (int64_t)b * a.per_part * a.N + (r - b * a.N);
+    const int b = quotient(r, a.N, a.by_n);
+    return r + (int64_t)b * (a.per_part - 1) * a.N;
 }
 
 template <int FR, int FS> struct Tile {
@@ -42,9 +51,9 @@ template <int FR, int FS> struct Tile {
     static constexpr int STAGE = (BR + BS) * BK;
 };
 
-// The place in LDS of 16-byte piece c (0 .. 3) of a 64-byte row: two rows share the 128 bytes that a clock delivers, and eight lanes with
-// consecutive rows read the same piece at once, so the piece is moved by bits 1 and 2 of the row: all eight come from banks of their own.
-__device__ __forceinline__ int piece_at(int row, int c) { return row * 64 + ((c ^ ((row >> 1) & 3)) << 4); }
+// The place in LDS of 16-byte piece c (0 .. 3) of a 64-byte row. A clock delivers 256 bytes, here the same piece of sixteen rows in a run: four rows
+// lie in 256 bytes, so the piece is moved by the row's number above that, and all sixteen come from banks of their own.
+__device__ __forceinline__ int piece_at(int row, int c) { return row * 64 + ((c ^ ((row >> 2) & 3)) << 4); }
 
 // 16 bytes of a row of K from column k on; what lies beyond K reads as zero.
 __device__ __forceinline__ uint4 load16(const int8_t *row, int64_t k, int64_t K)
@@ -71,7 +80,7 @@ __device__ __forceinline__ i32x16 mfma_i8(uint4 a, uint4 b, i32x16 c)
 template <typename T, int W> __device__ __forceinline__ void put(const LinArgs &a, int64_t col, int r, const T (&v)[W])
 {
     T *const y = (T *)a.y + col;
-    if (r + W <= a.nr && (!a.channels || r % a.N + W <= a.N)) {
+    if (r + W <= a.nr && (!a.channels || r - quotient(r, a.N, a.by_n) * a.N + W <= a.N)) {
         __builtin_memcpy(y + row_of(a, r), v, sizeof(v));
     } else {
 #pragma unroll
@@ -118,35 +127,35 @@ template <typename T> __device__ __forceinline__ void epilogue(const LinArgs &a,
     }
 }
 
-// The same inside y, with runs of rows that are neighbours in y: no conditions, and 16 bytes to each store. at[]: the places of this lane's runs of
-// rows (8 values of 16 bits: rows 8 half and 16 + 8 half; 4 of fp32: rows 8 j + 4 half).
-template <typename T> __device__ __forceinline__ void epilogue_whole(T *y, const i32x16 &acc, const f32x4 (&rs)[4], const f32x4 (&rb)[4], float ss, float sb,
-                                                                     const int64_t (&at)[sizeof(T)])
+// The same where a tile is inside y and its rows' runs of 16 bytes do not end within: by way of 4 KB of LDS of the wave's own, so that a store writes
+// 128 bytes in a row of eight columns, whole lines, instead of 32 of thirty-two. 64 rows (32 of fp32) of 32 columns at a time, a row of 128 bytes
+// to a column, its 16-byte pieces moved by the pair of columns; the halves of a piece change places in columns 16 up, so that the 32 lanes that
+// write at once meet no bank twice.
+template <typename T> __device__ __forceinline__ void scaled_to_lds(char *own, const i32x16 &acc, int part, const f32x4 (&rs)[4], const f32x4 (&rb)[4], float ss,
+                                                                    float sb)
 {
-    float v[16];
+    const int half = (threadIdx.x >> 5) & 1, l32 = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = fmaf((float)acc[i] * rs[i / 4][i % 4], ss, rb[i / 4][i % 4] + sb);
-    if constexpr (sizeof(T) == 4) {
+    for (int q = 0; q < 4; ++q) {
+        float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) __builtin_memcpy(y + at[j], v + 4 * j, 16);
-    } else {
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const T p[2] = {from_f32<T>(v[2 * i]), from_f32<T>(v[2 * i + 1])};
-            __builtin_memcpy(&w[i], p, 4);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-            uint32_t o[4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const auto x = __builtin_amdgcn_permlane32_swap(w[2 * j + i], w[2 * j + 2 + i], false, false);
-                o[i] = x[0], o[i + 2] = x[1];
-            }
-            __builtin_memcpy(y + at[j / 2], o, 16);
+        for (int i = 0; i < 4; ++i) v[i] = fmaf((float)acc[4 * q + i] * rs[q][i], ss, rb[q][i] + sb);
+        if constexpr (sizeof(T) == 4) {
+            *(float4 *)(own + l32 * 128 + (((2 * q + half) ^ ((l32 >> 1) & 7)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+            const T t[4] = {from_f32<T>(v[0]), from_f32<T>(v[1]), from_f32<T>(v[2]), from_f32<T>(v[3])};
+            uint2 w;
+            __builtin_memcpy(&w, t, 8);
+            *(uint2 *)(own + l32 * 128 + (((4 * part + q) ^ ((l32 >> 1) & 7)) << 4) + ((half ^ (l32 >> 4)) << 3)) = w;
         }
     }
+}
+// Piece (lane % 8) of column lane / 8 + 8 t of what lies there.
+template <typename T> __device__ __forceinline__ uint4 column_piece(const char *own, int t)
+{
+    const int lane = threadIdx.x & 63, c = (lane >> 3) + 8 * t;
+    const uint4 v = *(const uint4 *)(own + c * 128 + (((lane & 7) ^ ((c >> 1) & 7)) << 4));
+    return sizeof(T) == 2 && t >= 2 ? make_uint4(v.z, v.w, v.x, v.y) : v;
 }
 
 template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) k_linear(const LinArgs a)
@@ -266,7 +275,7 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) 
         base = (const char *)src + (int64_t)row0 * a.K - 3072;
 #pragma unroll
         for (int i = 0; i < LI; ++i) {
-            const int row = (wave & 3) * 16 * LI + i * 16 + (lane >> 2), piece = (lane & 3) ^ ((row >> 1) & 3);
+            const int row = (wave & 3) * 16 * LI + i * 16 + (lane >> 2), piece = (lane & 3) ^ ((row >> 2) & 3);
             off[i] = (uint32_t)(min(row0 + row, rows - 1) - row0) * (uint32_t)a.K + piece * 16 + 3072 - i * 1024;
         }
     };
@@ -274,7 +283,7 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) 
         if (tail && f_step == steps - 1) {                       // what lies beyond K reads as zeros
 #pragma unroll
             for (int i = 0; i < LI; ++i) {
-                const int piece = (lane & 3) ^ ((lane >> 3) & 3);
+                const int piece = (lane & 3) ^ ((lane >> 4) & 3);
                 const char *const from = base + off[i] + i * 1024;
                 to_lds16((int64_t)f_step * BK + piece * 16 < a.K ? from : (const char *)&zero_piece, lds + stage * STAGE + (wave * LI + i) * 1024);
             }
@@ -362,31 +371,59 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) 
         constexpr int W = 16 / sizeof(T);
         const bool whole = r0 + BR <= a.nr && s0 + BS <= a.ns && (!a.channels || a.N % W == 0);
         young = whole ? 2 : 0;
-#pragma unroll
-        for (int i = 0; i < FR; ++i) {
-            const int rbase = r0 + (wr * FR + i) * 32;
-            f32x4 rs[4], rb[4];
+        auto row_scales = [&](int i, f32x4 (&rs)[4], f32x4 (&rb)[4]) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 rs[q] = *(const f32x4 *)(sc + (i * 32 + 8 * q + 4 * half) * 4);
                 rb[q] = *(const f32x4 *)(sc + (NR * 64 + i * 32 + 8 * q + 4 * half) * 4);
             }
-            int64_t at[sizeof(T)];
-            if (whole) {
+        };
+        auto column_scale = [&](int j) { return *(const float *)(sc + (2 * NR * 64 + j * 32 + l32) * 4); };
+        auto column_bias = [&](int j) { return *(const float *)(sc + ((2 * NR + 1) * 64 + j * 32 + l32) * 4); };
+        bool done = false;
+        if constexpr (FR == 4) {                                 // (a stage has room for the waves; a smaller tile's has not)
+          if (whole) {
+            done = true;
+            // the stage of the last step, which nothing is on its way to yet
+            char *const mine = lds + (stage == 0 ? STAGES - 1 : stage - 1) * STAGE + wave * 4096;
+            constexpr int P = sizeof(T) == 2 ? 2 : 1;            // accumulators to a row of 128 bytes
+            static_assert(STAGE >= 8 * 4096, "room for the waves");
 #pragma unroll
-                for (int q = 0; q < (int)sizeof(T); ++q) at[q] = row_of(a, rbase + (sizeof(T) == 4 ? 8 * q + 4 * half : 16 * q + 8 * half));
+            for (int i = 0; i < FR; i += P) {
+                const int64_t row = row_of(a, r0 + (wr * FR + i) * 32 + (lane & 7) * W);
+                T *const y = (T *)a.y + row;
+#pragma unroll
+                for (int j = 0; j < FS; ++j) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const float ss = column_scale(j), sb = column_bias(j);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        f32x4 rs[4], rb[4];
+                        row_scales(i + p, rs, rb);
+                        scaled_to_lds<T>(mine, acc[i + p][j], p, rs, rb, ss, sb);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const uint4 v = column_piece<T>(mine, t);
+                        __builtin_memcpy(y + column_of(a, s0 + (wsv * FS + j) * 32 + (lane >> 3) + 8 * t), &v, 16);
+                    }
+                }
             }
+          }
+        }
+        if (!done) {
 #pragma unroll
-            for (int j = 0; j < FS; ++j) {
-                const int s = s0 + (wsv * FS + j) * 32 + l32;
-                const float ss = *(const float *)(sc + (2 * NR * 64 + j * 32 + l32) * 4), sb = *(const float *)(sc + ((2 * NR + 1) * 64 + j * 32 + l32) * 4);
-                if (whole) {
-                    epilogue_whole<T>((T *)a.y + column_of(a, s), acc[i][j], rs, rb, ss, sb, at);
-                } else {
-                    float rsv[16], rbv[16];
+            for (int i = 0; i < FR; ++i) {
+                f32x4 rs[4], rb[4];
+                row_scales(i, rs, rb);
+                float rsv[16], rbv[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) rsv[e] = rs[e / 4][e % 4], rbv[e] = rb[e / 4][e % 4];
-                    epilogue<T>(a, acc[i][j], rbase, s, rsv, rbv, ss, sb, column_of(a, min(s, a.ns - 1)));
+                for (int e = 0; e < 16; ++e) rsv[e] = rs[e / 4][e % 4], rbv[e] = rb[e / 4][e % 4];
+#pragma unroll
+                for (int j = 0; j < FS; ++j) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int s = s0 + (wsv * FS + j) * 32 + l32;
+                    epilogue<T>(a, acc[i][j], r0 + (wr * FR + i) * 32, s, rsv, rbv, column_scale(j), column_bias(j), column_of(a, min(s, a.ns - 1)));
                 }
             }
         }
@@ -471,6 +508,7 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
     (a.channels ? a.sbias : a.rbias) = bias;
     a.y = y, a.K = K, a.nr = (int)(a.channels ? t : O), a.ns = (int)(a.channels ? O : t);
     a.N = (int)N, a.per_part = (int)(parts ? O / parts : O), a.B = B;
+    a.by_n = reciprocal(a.N), a.by_part = reciprocal(a.per_part);
     auto launch = [&](auto fr, auto fs) -> int {
         constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value;
         using G = Tile<FR, FS>;

@@ -350,8 +350,8 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
     const int first = range * a.per, last = min(first + a.per, a.blocks);
 
     // What this lane brings to LDS. dy (b, n, o): rows of BO channels of a sample, their 16-byte pieces moved in pairs by the sample, so that the
-    // four samples of a transposing read lie in banks of their own. dy (b, o, n): rows of 64 samples of a channel, pieces moved by the channel.
-    // q: rows of 64 bytes, pieces moved by bits 1-2 of the channel. Channels beyond the end read others: what comes of them is not stored.
+    // four samples of a transposing read lie in banks of their own. dy (b, o, n): rows of 64 samples of a channel, pieces moved by
+    // the pair of channels (256 bytes, what a clock delivers). q: rows of 64 bytes, pieces moved by the four channels. Channels beyond the end read others: what comes of them is not stored.
     constexpr int LR = BO / 8;                                   // lanes to a row of (b, n, o)
     uint32_t aat[FO], bat[FC];
     int an[FO], bn[FC];                                          // this lane's first sample
@@ -363,14 +363,14 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
             an[i] = n;
             aat[i] = ((uint32_t)n * (uint32_t)a.O + (o0 + piece * 8 < a.O ? piece * 8 : 0)) * 2;
         } else {
-            const int o = p >> 3, piece = (p & 7) ^ (o & 7);
+            const int o = p >> 3, piece = (p & 7) ^ ((o >> 1) & 7);
             an[i] = piece * 8;
             aat[i] = ((uint32_t)(min(o0 + o, a.O - 1) - o0) * (uint32_t)a.N + piece * 8) * 2;
         }
     }
 #pragma unroll
     for (int i = 0; i < FC; ++i) {
-        const int p = (wave * FC + i) * 64 + lane, c = p >> 2, piece = (p & 3) ^ ((c >> 1) & 3);
+        const int p = (wave * FC + i) * 64 + lane, c = p >> 2, piece = (p & 3) ^ ((c >> 2) & 3);
         bn[i] = piece * 16;
         bat[i] = (uint32_t)(min(c0 + c, a.C - 1) - c0) * (uint32_t)a.N + piece * 16;
     }
@@ -426,9 +426,9 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
             ra[i] = (16 * half + m) * BO * 2 + piece * 16 + (j & 1) * 8;
         }
     } else {
-        ra[0] = (wo * FO * 32 + l32) * 128 + (((2 * half) ^ (l32 & 7)) << 4);
+        ra[0] = (wo * FO * 32 + l32) * 128 + (((2 * half) ^ ((l32 >> 1) & 7)) << 4);
     }
-    const int rq = Q_AT + (wc * FC * 32 + l32) * 64 + ((half ^ ((l32 >> 1) & 3)) << 4);
+    const int rq = Q_AT + (wc * FC * 32 + l32) * 64 + ((half ^ ((l32 >> 2) & 3)) << 4);
 
     // The operands of the products of a half run, in four groups 2 u + v: of dy one group ahead of its products, of q a pair of groups.
     uint4 fo[2][FO], fc[2][FC][2], raw[FC];
