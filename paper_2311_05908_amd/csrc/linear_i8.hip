@@ -131,15 +131,22 @@ template <typename T> __device__ __forceinline__ void epilogue(const LinArgs &a,
 // 128 bytes in a row of eight columns, whole lines, instead of 32 of thirty-two. 64 rows (32 of fp32) of 32 columns at a time, a row of 128 bytes
 // to a column, its 16-byte pieces moved by the pair of columns; the halves of a piece change places in columns 16 up, so that the 32 lanes that
 // write at once meet no bank twice.
-template <typename T> __device__ __forceinline__ void scaled_to_lds(char *own, const i32x16 &acc, int part, const f32x4 (&rs)[4], const f32x4 (&rb)[4], float ss,
-                                                                    float sb)
+template <typename T, bool CHANNELS> __device__ __forceinline__ void scaled_to_lds(char *own, const i32x16 &acc, int part, const float *rscale,
+                                                                                   const float *rbias, float ss, float sb)
 {
     const int half = (threadIdx.x >> 5) & 1, l32 = threadIdx.x & 31;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         float v[4];
+        const f32x4 rs = *(const f32x4 *)(rscale + 8 * q + 4 * half);
+        if constexpr (CHANNELS) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = fmaf((float)acc[4 * q + i] * rs[q][i], ss, rb[q][i] + sb);
+            for (int i = 0; i < 4; ++i) v[i] = fmaf((float)acc[4 * q + i] * rs[i], ss, sb);
+        } else {
+            const f32x4 rb = *(const f32x4 *)(rbias + 8 * q + 4 * half);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = fmaf((float)acc[4 * q + i] * rs[i], ss, rb[i]);
+        }
         if constexpr (sizeof(T) == 4) {
             *(float4 *)(own + l32 * 128 + (((2 * q + half) ^ ((l32 >> 1) & 7)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
         } else {
@@ -245,7 +252,7 @@ struct Walk {
     }
 };
 
-template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) k_linear_async(const LinArgs a, const Walk walk)
+template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bounds__(512, 2) k_linear_async(const LinArgs a, const Walk walk)
 {
     constexpr int BR = 64 * FR, BS = 128 * FS, BK = 64, STAGE = (BR + BS) * BK, STAGES = 4, LI = (BR + BS) / 128;
     static_assert(BR == BS, "waves 0-3 bring R, 4-7 bring S");
@@ -312,7 +319,7 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) 
         for (int j = 0; j < FS; ++j) fs[kk][j] = *(const uint4 *)(stage + (so ^ (kk << 5)) + j * 2048);
     };
     // Scales and biases of this wave's rows of a tile come to LDS at the tile's beginning, to a place of the wave's own, two tiles in turn.
-    constexpr int NR = FR / 2, PRIVATE = (2 * NR + 2) * 256, SCALES = 2 * NR + 2;
+    constexpr int NR = FR / 2, PRIVATE = (2 * NR + 2) * 256, SCALES = CHANNELS ? NR + 2 : 2 * NR + 1;
     const char *const own = lds + STAGES * STAGE + wave * 2 * PRIVATE;
     int tr, ts, parity = 0;
     auto fetch_scales = [&] {
@@ -323,10 +330,10 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) 
         for (int i = 0; i < NR; ++i) {
             const uint32_t o = (uint32_t)min(r + i * 64, a.nr - 1) * 4u;
             to_lds4(uniform((const char *)a.rscale), o, at + i * 256);
-            to_lds4(uniform(a.rbias ? (const char *)a.rbias : zero), a.rbias ? o : 0, at + (NR + i) * 256);
+            if (!CHANNELS) to_lds4(uniform(a.rbias ? (const char *)a.rbias : zero), a.rbias ? o : 0, at + (NR + i) * 256);
         }
         to_lds4(uniform((const char *)a.sscale), (uint32_t)sc * 4u, at + 2 * NR * 256);
-        to_lds4(uniform(a.sbias ? (const char *)a.sbias : zero), a.sbias ? (uint32_t)sc * 4u : 0, at + (2 * NR + 1) * 256);
+        if (CHANNELS) to_lds4(uniform(a.sbias ? (const char *)a.sbias : zero), a.sbias ? (uint32_t)sc * 4u : 0, at + (2 * NR + 1) * 256);
     };
     constexpr int STORES = FR * FS * (sizeof(T) == 4 ? 4 : 2);   // of a whole tile, at least
     FC_ARRIVED(2 * LI);
@@ -367,63 +374,62 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(512, 2) 
         if (steps < 3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const char *const sc = own + parity * PRIVATE;
         parity ^= 1;
-        const int r0 = tr * BR, s0 = ts * BS;
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));                         // (else the compiler keeps the places below in registers throughout the sums)
+        const int l32 = lane & 31, half = lane >> 5, r0 = tr * BR, s0 = ts * BS;
         constexpr int W = 16 / sizeof(T);
-        const bool whole = r0 + BR <= a.nr && s0 + BS <= a.ns && (!a.channels || a.N % W == 0);
-        young = whole ? 2 : 0;
-        auto row_scales = [&](int i, f32x4 (&rs)[4], f32x4 (&rb)[4]) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                rs[q] = *(const f32x4 *)(sc + (i * 32 + 8 * q + 4 * half) * 4);
-                rb[q] = *(const f32x4 *)(sc + (NR * 64 + i * 32 + 8 * q + 4 * half) * 4);
-            }
-        };
+        // All of it inside y, in one sequence and one part of y: places are linear in rows and columns.
+        bool whole = r0 + BR <= a.nr && s0 + BS <= a.ns && (CHANNELS ? a.N : a.nr) < 1 << 26;        // (32-bit distances of seven columns)
+        if (CHANNELS)
+            whole = whole && quotient(r0, a.N, a.by_n) == quotient(r0 + BR - 1, a.N, a.by_n) &&
+                    quotient(s0, a.per_part, a.by_part) == quotient(s0 + BS - 1, a.per_part, a.by_part);
+        young = 0;
         auto column_scale = [&](int j) { return *(const float *)(sc + (2 * NR * 64 + j * 32 + l32) * 4); };
         auto column_bias = [&](int j) { return *(const float *)(sc + ((2 * NR + 1) * 64 + j * 32 + l32) * 4); };
         bool done = false;
         if constexpr (FR == 4) {                                 // (a stage has room for the waves; a smaller tile's has not)
-          if (whole) {
-            done = true;
-            // the stage of the last step, which nothing is on its way to yet
-            char *const mine = lds + (stage == 0 ? STAGES - 1 : stage - 1) * STAGE + wave * 4096;
-            constexpr int P = sizeof(T) == 2 ? 2 : 1;            // accumulators to a row of 128 bytes
             static_assert(STAGE >= 8 * 4096, "room for the waves");
+            if (whole) {
+                done = true, young = 2;
+                // the stage of the last step, which nothing is on its way to yet
+                char *const mine = lds + (stage == 0 ? STAGES - 1 : stage - 1) * STAGE + wave * 4096;
+                constexpr int P = sizeof(T) == 2 ? 2 : 1;        // accumulators to a row of 128 bytes
+                const uint32_t stride = CHANNELS ? (uint32_t)a.N : (uint32_t)a.nr;
+                const int r1 = r0 + wr * FR * 32, s1 = s0 + wsv * FS * 32;
+                const char *const y = uniform((const char *)((T *)a.y + column_of(a, s1) + row_of(a, r1)));
+                const uint32_t at = ((uint32_t)(lane >> 3) * stride + (lane & 7) * W) * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int i = 0; i < FR; i += P) {
-                const int64_t row = row_of(a, r0 + (wr * FR + i) * 32 + (lane & 7) * W);
-                T *const y = (T *)a.y + row;
+                for (int i = 0; i < FR; i += P)
 #pragma unroll
-                for (int j = 0; j < FS; ++j) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    const float ss = column_scale(j), sb = column_bias(j);
+                    for (int j = 0; j < FS; ++j) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        const float ss = column_scale(j), sb = CHANNELS ? column_bias(j) : 0.f;
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        f32x4 rs[4], rb[4];
-                        row_scales(i + p, rs, rb);
-                        scaled_to_lds<T>(mine, acc[i + p][j], p, rs, rb, ss, sb);
+                        for (int p = 0; p < P; ++p)
+                            scaled_to_lds<T, CHANNELS>(mine, acc[i + p][j], p, (const float *)sc + (i + p) * 32, (const float *)sc + NR * 64 + (i + p) * 32, ss, sb);
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const uint4 v = column_piece<T>(mine, t);
+                            char *const to = (char *)y + ((int64_t)(j * 32 + 8 * t) * stride + i * 32) * (int)sizeof(T) + at;
+                            __builtin_memcpy(__builtin_assume_aligned(to, sizeof(T)), &v, 16);
+                        }
                     }
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const uint4 v = column_piece<T>(mine, t);
-                        __builtin_memcpy(y + column_of(a, s0 + (wsv * FS + j) * 32 + (lane >> 3) + 8 * t), &v, 16);
-                    }
-                }
             }
-          }
         }
         if (!done) {
 #pragma unroll
             for (int i = 0; i < FR; ++i) {
-                f32x4 rs[4], rb[4];
-                row_scales(i, rs, rb);
                 float rsv[16], rbv[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) rsv[e] = rs[e / 4][e % 4], rbv[e] = rb[e / 4][e % 4];
+                for (int e = 0; e < 16; ++e) {
+                    const int r = i * 32 + 8 * (e / 4) + 4 * half + e % 4;
+                    rsv[e] = ((const float *)sc)[r], rbv[e] = CHANNELS ? 0.f : ((const float *)sc)[NR * 64 + r];
+                }
 #pragma unroll
                 for (int j = 0; j < FS; ++j) {
                     __builtin_amdgcn_sched_barrier(0);
                     const int s = s0 + (wsv * FS + j) * 32 + l32;
-                    epilogue<T>(a, acc[i][j], r0 + (wr * FR + i) * 32, s, rsv, rbv, column_scale(j), column_bias(j), column_of(a, min(s, a.ns - 1)));
+                    epilogue<T>(a, acc[i][j], r0 + (wr * FR + i) * 32, s, rsv, rbv, column_scale(j), CHANNELS ? column_bias(j) : 0.f, column_of(a, min(s, a.ns - 1)));
                 }
             }
         }
@@ -521,7 +527,7 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
         constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value, BR = 64 * FR, BS = 128 * FS, lds = 4 * (BR + BS) * 64 + 16 * (FR + 2) * 256;
         a.tiles_r = (a.nr + BR - 1) / BR, a.tiles_s = (a.ns + BS - 1) / BS;
         Walk w = {a.tiles_s, a.tiles_s <= 12 ? a.tiles_s : 8, a.tiles_r * a.tiles_s};
-        const auto kernel = k_linear_async<T, FR, FS>;
+        const auto kernel = a.channels ? k_linear_async<T, true, FR, FS> : k_linear_async<T, false, FR, FS>;
         FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
         const int most = 256 * (FR == 4 ? 1 : 2);
         kernel<<<(unsigned)(w.tiles < most ? w.tiles : most), 512, lds, s>>>(a, w);
