@@ -17,6 +17,7 @@ struct LinArgs {
     int64_t K;
     int nr, ns;
     int channels;                 // y channel by channel: R is b * N + n, S is o
+    int beyond_cache;             // y is larger than the memory-side cache (256 MB) by far
     int N, per_part;              // samples of a sequence; output channels of a part
     uint32_t by_n, by_part;       // 2^32 over these, rounded up
     int64_t B;
@@ -156,6 +157,15 @@ template <typename T, bool CHANNELS> __device__ __forceinline__ void scaled_to_l
             *(uint2 *)(own + l32 * 128 + (((4 * part + q) ^ ((l32 >> 1) & 7)) << 4) + ((half ^ (l32 >> 4)) << 3)) = w;
         }
     }
+}
+// 16 bytes to y. Past the caches where y would only push everything else out of the memory-side one: bf16 64 x 4096 x 768 -> 3 x 768, 1.2 GB, 643 -> 619 us;
+// f16 8192 x 4096 -> 16384, 0.27 GB, 505 us with and 512 without them.
+template <bool BEYOND> __device__ __forceinline__ void put16(char *to, uint4 v)
+{
+    typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4;
+    const u32x4 w = {v.x, v.y, v.z, v.w};
+    if constexpr (BEYOND) __builtin_nontemporal_store(w, (u32x4 *)to);
+    else *(u32x4 *)to = w;
 }
 // Piece (lane % 8) of column lane / 8 + 8 t of what lies there.
 template <typename T> __device__ __forceinline__ uint4 column_piece(const char *own, int t)
@@ -319,7 +329,7 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
         for (int j = 0; j < FS; ++j) fs[kk][j] = *(const uint4 *)(stage + (so ^ (kk << 5)) + j * 2048);
     };
     // Scales and biases of this wave's rows of a tile come to LDS at the tile's beginning, to a place of the wave's own, two tiles in turn.
-    constexpr int NR = FR / 2, PRIVATE = (2 * NR + 2) * 256, SCALES = CHANNELS ? NR + 2 : 2 * NR + 1;
+    constexpr int NR = FR / 2, PRIVATE = (2 * NR + 2) * 256;
     const char *const own = lds + STAGES * STAGE + wave * 2 * PRIVATE;
     int tr, ts, parity = 0;
     auto fetch_scales = [&] {
@@ -335,10 +345,9 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
         to_lds4(uniform((const char *)a.sscale), (uint32_t)sc * 4u, at + 2 * NR * 256);
         if (CHANNELS) to_lds4(uniform(a.sbias ? (const char *)a.sbias : zero), a.sbias ? (uint32_t)sc * 4u : 0, at + (2 * NR + 1) * 256);
     };
-    constexpr int STORES = FR * FS * (sizeof(T) == 4 ? 4 : 2);   // of a whole tile, at least
     FC_ARRIVED(2 * LI);
     read(lds, 0);
-    int stage = 0, young = 0;                                    // steps at whose barrier the last tile's stores may still be on their way
+    int stage = 0;
     for (int tile = first; tile < last; tile += on_die) {
         walk.place(tile, tr, ts, a.tiles_r);
         fetch_scales();
@@ -356,14 +365,7 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
             __builtin_amdgcn_sched_barrier(0);
             products(0);
             __builtin_amdgcn_sched_barrier(0);
-            // The next step's pieces are there; those of the two after it may be on their way, and at a tile's first two steps the stores of the tile
-            // before it and its scales, which were sent off after the pieces that are waited for.
-            if (young) {
-                FC_ARRIVED(2 * LI + STORES + SCALES);
-                --young;
-            } else {
-                FC_ARRIVED(2 * LI);
-            }
+            FC_ARRIVED(2 * LI);                                  // the next step's pieces are there, those of the two after it on their way
             stage = stage + 1 < STAGES ? stage + 1 : 0;
             read(lds + stage * STAGE, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -383,14 +385,13 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
         if (CHANNELS)
             whole = whole && quotient(r0, a.N, a.by_n) == quotient(r0 + BR - 1, a.N, a.by_n) &&
                     quotient(s0, a.per_part, a.by_part) == quotient(s0 + BS - 1, a.per_part, a.by_part);
-        young = 0;
         auto column_scale = [&](int j) { return *(const float *)(sc + (2 * NR * 64 + j * 32 + l32) * 4); };
         auto column_bias = [&](int j) { return *(const float *)(sc + ((2 * NR + 1) * 64 + j * 32 + l32) * 4); };
         bool done = false;
         if constexpr (FR == 4) {                                 // (a stage has room for the waves; a smaller tile's has not)
             static_assert(STAGE >= 8 * 4096, "room for the waves");
             if (whole) {
-                done = true, young = 2;
+                done = true;
                 // the stage of the last step, which nothing is on its way to yet
                 char *const mine = lds + (stage == 0 ? STAGES - 1 : stage - 1) * STAGE + wave * 4096;
                 constexpr int P = sizeof(T) == 2 ? 2 : 1;        // accumulators to a row of 128 bytes
@@ -398,6 +399,7 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
                 const int r1 = r0 + wr * FR * 32, s1 = s0 + wsv * FS * 32;
                 const char *const y = uniform((const char *)((T *)a.y + column_of(a, s1) + row_of(a, r1)));
                 const uint32_t at = ((uint32_t)(lane >> 3) * stride + (lane & 7) * W) * (uint32_t)sizeof(T);
+                auto all = [&](auto beyond) {
 #pragma unroll
                 for (int i = 0; i < FR; i += P)
 #pragma unroll
@@ -411,9 +413,12 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
                         for (int t = 0; t < 4; ++t) {
                             const uint4 v = column_piece<T>(mine, t);
                             char *const to = (char *)y + ((int64_t)(j * 32 + 8 * t) * stride + i * 32) * (int)sizeof(T) + at;
-                            __builtin_memcpy(__builtin_assume_aligned(to, sizeof(T)), &v, 16);
+                            put16<decltype(beyond)::value>(to, v);
                         }
                     }
+                };
+                if (a.beyond_cache) all(std::true_type());
+                else all(std::false_type());
             }
         }
         if (!done) {
@@ -514,6 +519,7 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
     (a.channels ? a.sbias : a.rbias) = bias;
     a.y = y, a.K = K, a.nr = (int)(a.channels ? t : O), a.ns = (int)(a.channels ? O : t);
     a.N = (int)N, a.per_part = (int)(parts ? O / parts : O), a.B = B;
+    a.beyond_cache = t * O * (int64_t)sizeof(T) > (int64_t)512 << 20;
     a.by_n = reciprocal(a.N), a.by_part = reciprocal(a.per_part);
     auto launch = [&](auto fr, auto fs) -> int {
         constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value;

@@ -230,6 +230,23 @@ def test_products_in_8_bits(b, n, k, o, dtype, layout, parts):
         assert torch.equal(layers.linear_i8((xq[0], xs[0]), (wq, ws), dtype=DT[dtype]), y[0])
 
 
+@pytest.mark.parametrize("layout,parts,dtype", [("tokens", 1, "bf16"), ("channels", 1, "f16"), ("channels", 3, "bf16"), ("tokens", 1, "f32"), ("channels", 3, "f32")])
+@pytest.mark.parametrize("b,n,k,o", [(33, 512, 832, 1200), (7, 2600, 64, 3840), (1, 20011, 272, 1023), (3, 8192, 16, 768), (1, 19000, 100, 900)])
+def test_products_of_many_tiles(b, n, k, o, layout, parts, dtype):
+    """Several tiles to a workgroup: inside y and at its ends, across sequences and parts, of one step and of many, the last one short; every
+    output against the exact sums."""
+    g = gen(b + n + k + o)
+    xq, wq = int_rows(g, b, n, k), int_rows(g, o, k)
+    xs, ws = torch.rand(b, n, generator=g, device="cuda") + 0.01, (torch.rand(o, generator=g, device="cuda") + 0.01) / k
+    bias = normal(g, o)
+    sums = (xq.reshape(-1, k).float() @ wq.float().T).double() if k < 1000 else (xq.reshape(-1, k).double() @ wq.double().T)   # (below 2^24: exact)
+    ref = sums.reshape(b, n, o) * xs.double()[..., None] * ws.double()
+    bound = (U[dtype] + 4 * E) * (ref.abs() + bias.abs().double()) + TINY[dtype]
+    ref = ref + bias.double()
+    y = layers.linear_i8((xq, xs), (wq, ws), bias=bias, dtype=DT[dtype], layout=layout, parts=parts)
+    within(y, laid_out(ref, layout, parts), laid_out(bound, layout, parts))
+
+
 def test_products_at_the_largest_sums_and_offsets():
     """All factors -128 at the largest k; y and x beyond 2^31 values; scales that are zero or NaN reach their own rows alone."""
     k = 131071
