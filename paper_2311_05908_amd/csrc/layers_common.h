@@ -56,6 +56,21 @@ template <typename T, int E> __device__ __forceinline__ void store_rounded(T *p,
     store_piece<T, E>(p, left, raw);
 }
 
+// The same for rows whose length is a multiple of E: a piece is there or not (`left` is then 0 or below). One that is not is read at `row`'s beginning
+// and set to zero: no branch parts the loads, so all of a row's are on their way together.
+template <typename T, int E, bool WHOLE> __device__ __forceinline__ void load_row_piece(const T *row, int64_t col, int64_t D, float (&v)[E])
+{
+    if constexpr (WHOLE) {
+        const bool there = col < D;
+        T raw[E];
+        __builtin_memcpy(raw, row + (there ? col : 0), sizeof(raw));
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = there ? to_f32(raw[e]) : 0.f;
+    } else {
+        load_piece<T, E>(row + col, D - col, v);
+    }
+}
+
 // A magnitude as an integer: of two, the larger number is the larger integer, infinities are above every finite number and NaN above
 // infinities, so the largest of a row says whether anything in it is not finite.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }

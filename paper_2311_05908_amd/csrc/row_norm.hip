@@ -36,28 +36,29 @@ template <int WPR, typename F> __device__ __forceinline__ uint32_t row_reduce(ui
     return x;
 }
 
-template <typename T, int E, int CH, int WPR> __global__ void __launch_bounds__(WPR == 16 ? 1024 : 256) k_rows(const RowArgs a)
+template <typename T, int E, int CH, int WPR, bool WHOLE> __global__ void __launch_bounds__(WPR == 16 ? 1024 : 256) k_rows(const RowArgs a)
 {
     constexpr int LANES = 64 * WPR, ROWS = WPR == 1 ? 4 : 1;
     __shared__ uint32_t part[2][16];
     int at = 0;
     const int lane = threadIdx.x % LANES;
     const float by_d = 1.f / (float)a.D;
+    float w[CH][E];                                       // the norm's weight, for all of the workgroup's rows
+    if (a.norm) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) load_row_piece<float, E, WHOLE>(a.w, (int64_t)(lane + c * LANES) * E, a.D, w[c]);
+    }
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < a.T; row += (int64_t)gridDim.x * ROWS) {
         const T *const x = (const T *)a.x + row * a.ldx;
         const T *const r = a.r ? (const T *)a.r + row * a.ldr : nullptr;
         float v[CH][E];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int64_t col = (int64_t)(lane + c * LANES) * E;
-            load_piece<T, E>(x + col, a.D - col, v[c]);
-        }
+        for (int c = 0; c < CH; ++c) load_row_piece<T, E, WHOLE>(x, (int64_t)(lane + c * LANES) * E, a.D, v[c]);
         if (r) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int64_t col = (int64_t)(lane + c * LANES) * E;
                 float t[E];
-                load_piece<T, E>(r + col, a.D - col, t);
+                load_row_piece<T, E, WHOLE>(r, (int64_t)(lane + c * LANES) * E, a.D, t);
 #pragma unroll
                 for (int e = 0; e < E; ++e) v[c][e] += t[e];
             }
@@ -79,13 +80,9 @@ template <typename T, int E, int CH, int WPR> __global__ void __launch_bounds__(
             const float rstd = 1.f / sqrtf(fmaf(ss, by_d, a.eps));
             if (a.rstd && lane == 0) a.rstd[row] = rstd;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int64_t col = (int64_t)(lane + c * LANES) * E;
-                float w[E];
-                load_piece<float, E>(a.w + col, a.D - col, w);
+            for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[c][e] = v[c][e] * rstd * w[e];
-            }
+                for (int e = 0; e < E; ++e) v[c][e] = v[c][e] * rstd * w[c][e];
         }
         if (!a.i8) {
 #pragma unroll
@@ -122,7 +119,7 @@ struct NormGradArgs {
     int64_t T, D, lddy;
 };
 
-template <typename T, int E, int CH, int WPR> __global__ void __launch_bounds__(WPR == 16 ? 1024 : 256) k_norm_grad(const NormGradArgs a)
+template <typename T, int E, int CH, int WPR, bool WHOLE> __global__ void __launch_bounds__(WPR == 16 ? 1024 : 256) k_norm_grad(const NormGradArgs a)
 {
     constexpr int LANES = 64 * WPR, ROWS = WPR == 1 ? 4 : 1;
     __shared__ uint32_t part[2][16];
@@ -130,27 +127,30 @@ template <typename T, int E, int CH, int WPR> __global__ void __launch_bounds__(
     int at = 0;
     const int lane = threadIdx.x % LANES;
     const float by_d = 1.f / (float)a.D;
-    float dw[CH][E] = {};
+    float dw[CH][E] = {}, w[CH][E];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load_row_piece<float, E, WHOLE>(a.w, (int64_t)(lane + c * LANES) * E, a.D, w[c]);
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < a.T; row += (int64_t)gridDim.x * ROWS) {
-        float g[CH][E], z[CH][E];
+        float g[CH][E], z[CH][E], dh[CH][E] = {};
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int64_t col = (int64_t)(lane + c * LANES) * E;
-            load_piece<T, E>((const T *)a.dy + row * a.lddy + col, a.D - col, g[c]);
-            load_piece<T, E>((const T *)a.h + row * a.D + col, a.D - col, z[c]);
+            load_row_piece<T, E, WHOLE>((const T *)a.dy + row * a.lddy, col, a.D, g[c]);
+            load_row_piece<T, E, WHOLE>((const T *)a.h + row * a.D, col, a.D, z[c]);
         }
         const float rstd = a.rstd[row];
+        if (a.dh) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) load_row_piece<T, E, WHOLE>((const T *)a.dh + row * a.D, (int64_t)(lane + c * LANES) * E, a.D, dh[c]);
+        }
         float dot = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int64_t col = (int64_t)(lane + c * LANES) * E;
-            float w[E];
-            load_piece<float, E>(a.w + col, a.D - col, w);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 z[c][e] *= rstd;
                 dw[c][e] = fmaf(g[c][e], z[c][e], dw[c][e]);
-                g[c][e] *= w[e];
+                g[c][e] *= w[c][e];
                 dot = fmaf(g[c][e], z[c][e], dot);
             }
         }
@@ -158,10 +158,8 @@ template <typename T, int E, int CH, int WPR> __global__ void __launch_bounds__(
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int64_t col = (int64_t)(lane + c * LANES) * E;
-            float dh[E] = {};
-            if (a.dh) load_piece<T, E>((const T *)a.dh + row * a.D + col, a.D - col, dh);
 #pragma unroll
-            for (int e = 0; e < E; ++e) g[c][e] = fmaf(rstd, fmaf(-z[c][e], dot, g[c][e]), dh[e]);
+            for (int e = 0; e < E; ++e) g[c][e] = fmaf(rstd, fmaf(-z[c][e], dot, g[c][e]), dh[c][e]);
             store_rounded<T, E>((T *)a.dx + row * a.D + col, a.D - col, g[c]);
         }
     }
@@ -215,7 +213,7 @@ static RowShape row_shape(int64_t D, int dtype)
 template <typename F> static int with_row_kernel(int64_t D, int dtype, F f)
 {
     const RowShape s = row_shape(D, dtype);
-#define FC_ROW(TY, E_, CH_, W_) if (s.e == E_ && s.ch == CH_ && s.wpr == W_) return f(TY(), std::integral_constant<int, E_>(), std::integral_constant<int, CH_>(), std::integral_constant<int, W_>());
+#define FC_ROW(TY, E_, CH_, W_) if (s.e == E_ && s.ch == CH_ && s.wpr == W_) return D % E_ == 0 ? f(TY(), std::integral_constant<int, E_>(), std::integral_constant<int, CH_>(), std::integral_constant<int, W_>(), std::true_type()) : f(TY(), std::integral_constant<int, E_>(), std::integral_constant<int, CH_>(), std::integral_constant<int, W_>(), std::false_type());
 #define FC_ROW16(TY) FC_ROW(TY, 4, 1, 1) FC_ROW(TY, 4, 3, 1) FC_ROW(TY, 8, 1, 1) FC_ROW(TY, 8, 2, 1) FC_ROW(TY, 8, 3, 1) FC_ROW(TY, 8, 4, 1) \
         FC_ROW(TY, 8, 2, 4) FC_ROW(TY, 8, 3, 4) FC_ROW(TY, 8, 4, 4) FC_ROW(TY, 8, 2, 16)
     if (dtype == FFTCONV_BF16) {
@@ -234,11 +232,14 @@ template <typename F> static int with_row_kernel(int64_t D, int dtype, F f)
 
 static int64_t row_groups(int64_t T, const RowShape &s) { return s.wpr == 1 ? (T + 3) / 4 : T; }
 
+// Workgroups of the forward pass: enough to fill the chip, each with the weight in registers for all of its rows.
+constexpr int64_t MOST_GROUPS = 256 * 8;
+
 // Workgroups of the backward pass: each leaves a row of sums, so there are no more than fill the chip.
 static int64_t grad_groups(int64_t T, int64_t D, int dtype)
 {
     const RowShape s = row_shape(D, dtype);
-    const int64_t most = s.wpr == 1 ? 1024 : s.wpr == 4 ? 1024 : 512;
+    const int64_t most = s.wpr == 1 ? 1536 : s.wpr == 4 ? 1024 : 512;
     const int64_t g = row_groups(T, s);
     return g < 1 ? 1 : g < most ? g : most;                  // (no row: one workgroup writes dw's zeros)
 }
@@ -253,11 +254,11 @@ int rows_forward(const void *x, int64_t ldx, const void *r, int64_t ldr, const f
                  int64_t D, double eps, int norm, int i8, int dtype, hipStream_t s)
 {
     const RowArgs a = {x, r, w, y, h, rstd, scale, T, D, ldx, ldr, (float)eps, norm, i8};
-    return with_row_kernel(D, dtype, [&](auto t, auto e, auto ch, auto wpr) -> int {
+    return with_row_kernel(D, dtype, [&](auto t, auto e, auto ch, auto wpr, auto whole) -> int {
         using TY = decltype(t);
         int64_t g = row_groups(T, row_shape(D, dtype));
-        if (g > (1 << 30)) g = 1 << 30;
-        k_rows<TY, decltype(e)::value, decltype(ch)::value, decltype(wpr)::value><<<(unsigned)g, decltype(wpr)::value == 16 ? 1024 : 256, 0, s>>>(a);
+        if (g > MOST_GROUPS) g = MOST_GROUPS;
+        k_rows<TY, decltype(e)::value, decltype(ch)::value, decltype(wpr)::value, decltype(whole)::value><<<(unsigned)g, decltype(wpr)::value == 16 ? 1024 : 256, 0, s>>>(a);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     });
@@ -268,9 +269,9 @@ int rms_norm_backward(const void *dy, int64_t lddy, const void *h, const void *d
 {
     const int64_t groups = grad_groups(T, D, dtype);
     const NormGradArgs a = {dy, h, dh, w, rstd, dx, groups > 1 ? (float *)workspace : dw, T, D, lddy};
-    FC_TRY(with_row_kernel(D, dtype, [&](auto t, auto e, auto ch, auto wpr) -> int {
+    FC_TRY(with_row_kernel(D, dtype, [&](auto t, auto e, auto ch, auto wpr, auto whole) -> int {
         using TY = decltype(t);
-        k_norm_grad<TY, decltype(e)::value, decltype(ch)::value, decltype(wpr)::value><<<(unsigned)groups, decltype(wpr)::value == 16 ? 1024 : 256, 0, s>>>(a);
+        k_norm_grad<TY, decltype(e)::value, decltype(ch)::value, decltype(wpr)::value, decltype(whole)::value><<<(unsigned)groups, decltype(wpr)::value == 16 ? 1024 : 256, 0, s>>>(a);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     }));

@@ -165,6 +165,11 @@ def _stream_ptr():
     return _raw_stream(_current_device())
 
 
+def _extension():
+    """The binding's extension; raises ImportError where it is not built."""
+    return importlib.import_module("._fastcall", __package__)
+
+
 @functools.lru_cache(maxsize=None)
 def _fastcall():
     """call() of the binding's extension, which is built first if there is none; None where it cannot be."""
@@ -172,7 +177,7 @@ def _fastcall():
         _build.try_build_fastcall()
         importlib.invalidate_caches()
     try:
-        return importlib.import_module("._fastcall", __package__).call
+        return _extension().call
     except ImportError:
         return None
 

@@ -154,3 +154,30 @@ def test_the_binding_refuses_what_the_library_would_misread():
         layers.rms_norm(torch.zeros(1, 8, device=d).expand(4, 8), w)          # rows on top of each other
     with pytest.raises(fftconv.FFTConvError):
         layers.rms_norm(torch.zeros(1, 16385, device=d), torch.ones(16385, device=d))
+
+
+def test_the_extension_passes_a_norms_arguments():
+    """Thirteen integers with a double among them, through the call that the norm is made with; refused in other numbers or kinds."""
+    from paper_2311_05908_amd import build
+
+    if build.build_fastcall() is None:
+        pytest.skip("no Python headers")
+    from paper_2311_05908_amd import _fastcall
+
+    seen = []
+    i64 = [ctypes.c_int64]
+    f = ctypes.CFUNCTYPE(ctypes.c_int, *i64 * 11, ctypes.c_double, *i64 * 2)(lambda *a: seen.append(a) or -3)
+    address = ctypes.cast(f, ctypes.c_void_p).value
+    given = [0x7f1234567890, -1, None, 0, 5, 6, None, 8, 9, 1 << 40, 11, 2, 0x7f0000000010]
+    assert _fastcall.call_norm(address, 1e-6, *given) == -3
+    want = [x or 0 for x in given]
+    assert seen == [(*want[:11], 1e-6, *want[11:])]
+    for bad in ([1e-6, *given[:-1]], [1e-6, *given, 0], ["x", *given], [None, *given], [1e-6, *given[:-1], 1.5], [1e-6, *given[:-1], 1 << 64]):
+        with pytest.raises((TypeError, OverflowError)):
+            _fastcall.call_norm(address, *bad)
+    with pytest.raises(ValueError):
+        _fastcall.call_norm(0, 1e-6, *given)
+    for n in (13, 14):
+        seen.clear()
+        g = ctypes.CFUNCTYPE(ctypes.c_int, *i64 * n)(lambda *a: seen.append(a) or n)
+        assert _fastcall.call(ctypes.cast(g, ctypes.c_void_p).value, *range(1, n + 1)) == n and seen == [tuple(range(1, n + 1))]
