@@ -10,24 +10,43 @@
 namespace fftconv {
 namespace lay {
 
-// A run is 16 lanes of 8 values: one piece a lane, the largest magnitude from exchanges inside a row of 16 lanes.
-template <typename T> __global__ void __launch_bounds__(256) k_pack(const T *__restrict__ x, int8_t *__restrict__ q, float *__restrict__ scale,
-                                                                     int64_t total, int64_t runs, int64_t N)
+// A run is 16 lanes of 8 values: one piece a lane, the largest magnitude from exchanges inside a row of 16 lanes. A workgroup takes 16 R runs, each
+// lane R pieces at once. WHOLE: samples in runs, so that a tensor is one long row and nothing has to be divided.
+template <typename T, bool WHOLE> __device__ __forceinline__ bool run_at(int64_t i, int64_t total, int64_t runs, int64_t N, int64_t &at, int64_t &left)
 {
     const int l = threadIdx.x & 15;
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += (int64_t)gridDim.x * 16) {
-        const int64_t row = i / runs, n = (i - row * runs) * RUN + l * 8, left = N - n;
-        float v[8];
-        load_piece<T, 8>(x + row * N + n, left, v);
+    if (WHOLE) {
+        at = i * RUN + l * 8, left = RUN;
+    } else {
+        const int64_t row = i / runs, n = (i - row * runs) * RUN + l * 8;
+        at = row * N + n, left = N - n;
+    }
+    return i < total;
+}
+
+template <typename T, bool WHOLE> __global__ void __launch_bounds__(256) k_pack(const T *__restrict__ x, int8_t *__restrict__ q, float *__restrict__ scale,
+                                                                                int64_t total, int64_t runs, int64_t N)
+{
+    constexpr int R = 2;
+    const int64_t i0 = (int64_t)blockIdx.x * 16 * R + (threadIdx.x >> 4);
+    float v[R][8];
+    int64_t at[R], left[R];
+    bool there[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        there[r] = run_at<T, WHOLE>(i0 + r * 16, total, runs, N, at[r], left[r]);
+        load_piece<T, 8>(x + at[r], there[r] ? left[r] : 0, v[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
         uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = MaxU32()(top, magnitude(v[e]));
+        for (int e = 0; e < 8; ++e) top = MaxU32()(top, magnitude(v[r][e]));
         const float s = scale_of(reduce16(top, MaxU32()));
         int8_t o[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = quantised(v[e], s);
-        store_piece<int8_t, 8>(q + row * N + n, left, o);
-        if (l == 0) scale[i] = s;
+        quantise<8>(v[r], s, o);
+        store_piece<int8_t, 8>(q + at[r], there[r] ? left[r] : 0, o);
+        if (there[r] && (threadIdx.x & 15) == 0) scale[i0 + r * 16] = s;
     }
 }
 
@@ -82,30 +101,35 @@ template <typename T> __global__ void __launch_bounds__(256) k_pack_tokens(const
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(256) k_unpack(const int8_t *__restrict__ q, const float *__restrict__ scale,
-                                                                       const int8_t *__restrict__ gq, const float *__restrict__ gscale,
-                                                                       const T *__restrict__ gate, T *__restrict__ x, int64_t total, int64_t runs,
-                                                                       int64_t N)
+template <typename T, bool WHOLE> __global__ void __launch_bounds__(256) k_unpack(const int8_t *__restrict__ q, const float *__restrict__ scale,
+                                                                                  const int8_t *__restrict__ gq, const float *__restrict__ gscale,
+                                                                                  const T *__restrict__ gate, T *__restrict__ x, int64_t total,
+                                                                                  int64_t runs, int64_t N)
 {
-    const int l = threadIdx.x & 15;
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += (int64_t)gridDim.x * 16) {
-        const int64_t row = i / runs, n = (i - row * runs) * RUN + l * 8, left = N - n, at = row * N + n;
-        float v[8], g[8];
-        load_piece<int8_t, 8>(q + at, left, v);
-        const float s = scale[i];
+    constexpr int R = 2;
+    const int64_t i0 = (int64_t)blockIdx.x * 16 * R + (threadIdx.x >> 4);
+    float v[R][8], g[R][8], s[R], gs[R];
+    int64_t at[R], left[R];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= s;
-        if (gq) {
-            load_piece<int8_t, 8>(gq + at, left, g);
-            const float gs = gscale[i];
+    for (int r = 0; r < R; ++r) {
+        const int64_t i = i0 + r * 16;
+        const bool there = run_at<T, WHOLE>(i, total, runs, N, at[r], left[r]);
+        left[r] = there ? left[r] : 0;
+        load_piece<int8_t, 8>(q + at[r], left[r], v[r]);
+        s[r] = there ? scale[i] : 0.f;
+        gs[r] = there && gq ? gscale[i] : 1.f;
+        if (gq) load_piece<int8_t, 8>(gq + at[r], left[r], g[r]);
+        else if (gate) load_piece<T, 8>(gate + at[r], left[r], g[r]);
+    }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= g[e] * gs;
-        } else if (gate) {
-            load_piece<T, 8>(gate + at, left, g);
+    for (int r = 0; r < R; ++r) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= g[e];
+        for (int e = 0; e < 8; ++e) v[r][e] *= s[r];
+        if (gq || gate) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[r][e] *= g[r][e] * gs[r];
         }
-        store_rounded<T, 8>(x + at, left, v);
+        store_rounded<T, 8>(x + at[r], left[r], v[r]);
     }
 }
 
@@ -128,7 +152,9 @@ int act_pack(const void *x, int8_t *q, float *scale, int64_t B, int64_t C, int64
             k_pack_tokens<T><<<groups_of(total), 256, 0, s>>>((const T *)x, q, scale, C, N, runs, cg, total);
         } else {
             const int64_t total = B * C * runs;
-            k_pack<T><<<groups_of((total + 15) / 16), 256, 0, s>>>((const T *)x, q, scale, total, runs, N);
+            const unsigned g = (unsigned)((total + 31) / 32);
+            if (N % RUN == 0) k_pack<T, true><<<g, 256, 0, s>>>((const T *)x, q, scale, total, runs, N);
+            else k_pack<T, false><<<g, 256, 0, s>>>((const T *)x, q, scale, total, runs, N);
         }
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
@@ -141,7 +167,9 @@ int act_unpack(const int8_t *q, const float *scale, const int8_t *gq, const floa
     const int64_t runs = (N + RUN - 1) / RUN, total = B * C * runs;
     return with_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
-        k_unpack<T><<<groups_of((total + 15) / 16), 256, 0, s>>>(q, scale, gq, gscale, (const T *)gate, (T *)x, total, runs, N);
+        const unsigned g = (unsigned)((total + 31) / 32);
+        if (N % RUN == 0) k_unpack<T, true><<<g, 256, 0, s>>>(q, scale, gq, gscale, (const T *)gate, (T *)x, total, runs, N);
+        else k_unpack<T, false><<<g, 256, 0, s>>>(q, scale, gq, gscale, (const T *)gate, (T *)x, total, runs, N);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     });

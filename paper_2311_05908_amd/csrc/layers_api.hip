@@ -38,6 +38,10 @@ int check_acts(const char *who, int64_t B, int64_t C, int64_t N, int dtype)
     if (!known(dtype)) return bad(who, "unknown dtype");
     if (B < 0 || C < 1 || N < 1) return bad(who, "B >= 0, C >= 1 and N >= 1 are wanted");
     if (times(B, C, INT64_MAX / 64) < 0 || times(times(B, C, INT64_MAX / 64), N, INT64_MAX / 64) < 0) return bad(who, "too many values");
+    if (times(times(B, C, INT64_MAX / 64), (N + 127) / 128, INT64_MAX / 64) > (int64_t)1 << 35) {
+        set_error("%s: over 2^35 runs of 128 samples", who);
+        return FFTCONV_EUNSUPPORTED;
+    }
     return FFTCONV_OK;
 }
 

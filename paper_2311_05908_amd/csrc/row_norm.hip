@@ -104,8 +104,7 @@ template <typename T, int E, int CH, int WPR, bool WHOLE> __global__ void __laun
         for (int c = 0; c < CH; ++c) {
             const int64_t col = (int64_t)(lane + c * LANES) * E;
             int8_t q[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) q[e] = quantised(v[c][e], s);
+            quantise<E>(v[c], s, q);
             store_piece<int8_t, E>((int8_t *)a.y + row * a.D + col, a.D - col, q);
         }
     }
