@@ -119,7 +119,7 @@ int fftconv_rms_norm_backward(const void *dy, int64_t lddy, const void *h, const
 size_t fftconv_workspace_bytes_linear_i8(int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype)
 {
     if (B < 1 || check_linear("fftconv_workspace_bytes_linear_i8", B, N, K, O, parts, dtype) != FFTCONV_OK) return 0;
-    return lay::linear_i8_workspace(B * N, K, O, parts);
+    return lay::linear_i8_workspace(B * N, K, O);
 }
 
 int fftconv_linear_i8(const int8_t *x, const float *x_scale, const int8_t *w, const float *w_scale, const float *bias, void *y, int64_t B,

@@ -25,7 +25,7 @@ int act_unpack(const int8_t *q, const float *scale, const int8_t *gq, const floa
                int64_t N, int dtype, hipStream_t s);
 
 // linear_i8.hip
-size_t linear_i8_workspace(int64_t T, int64_t K, int64_t O, int64_t parts);
+size_t linear_i8_workspace(int64_t T, int64_t K, int64_t O);
 int linear_i8(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, void *y, int64_t B, int64_t N, int64_t K,
               int64_t O, int64_t parts, int dtype, void *workspace, hipStream_t s);
 

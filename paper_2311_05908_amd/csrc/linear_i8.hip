@@ -22,6 +22,8 @@ struct LinArgs {
     uint32_t by_n, by_part;       // 2^32 over these, rounded up
     int64_t B;
     int tiles_r, tiles_s;
+    int ranges, per;              // of k, whose sums of a tile are added up by a second kernel (1: all of k); steps of one
+    int *part;                    // (ranges, ns, nr)
 };
 
 // x / d for 0 <= x < 2^31 from the reciprocal: at most one too large before the correction.
@@ -262,7 +264,7 @@ struct Walk {
     }
 };
 
-template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bounds__(512, 2) k_linear_async(const LinArgs a, const Walk walk)
+template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void __launch_bounds__(512, 2) k_linear_async(const LinArgs a, const Walk walk)
 {
     constexpr int BR = 64 * FR, BS = 128 * FS, BK = 64, STAGE = (BR + BS) * BK, STAGES = 4, LI = (BR + BS) / 128;
     static_assert(BR == BS, "waves 0-3 bring R, 4-7 bring S");
@@ -273,8 +275,14 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
     const int wgs = gridDim.x, die = blockIdx.x % 8, dies = min(8, wgs), on_die = (wgs - die + 7) / 8;
     const int begin = (int)((int64_t)walk.tiles * die / dies), last = (int)((int64_t)walk.tiles * (die + 1) / dies);
     const int first = begin + blockIdx.x / 8;
-    const int steps = (int)((a.K + BK - 1) / BK);
+    const int all_steps = (int)((a.K + BK - 1) / BK);
     const bool tail = a.K % BK != 0;
+    // item i of the walk: tile i / ranges, range i % ranges of k
+    auto item = [&](int i, int &tr, int &ts, int &range) {
+        range = SPLIT ? i % a.ranges : 0;
+        walk.place(SPLIT ? i / a.ranges : i, tr, ts, a.tiles_r);
+    };
+    auto steps_of = [&](int range) { return SPLIT ? min(a.per, all_steps - range * a.per) : all_steps; };
 
     // This wave brings rows 16 LI w' ... of R (waves 0-3) or S (4-7), sixteen with an instruction, a piece of 16 bytes for each lane, moved as
     // piece_at has it.
@@ -282,14 +290,15 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
     const int8_t *const src = is_r ? a.r : a.s;
     const int rows = is_r ? a.nr : a.ns, block = is_r ? BR : BS;
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * LI * 1024;
-    int f_tile = first, f_step = 0;                              // what is asked for next
+    int f_tile = first, f_step = 0, f_steps = 0, f_first = 0;    // what is asked for next; steps of its range, and of those before it
     const char *base = nullptr;
     uint32_t off[LI];
     auto aim = [&] {                                             // at tile f_tile, or, after the last, once more at it
-        int tr, ts;
-        walk.place(min(f_tile, last - 1), tr, ts, a.tiles_r);
+        int tr, ts, range;
+        item(min(f_tile, last - 1), tr, ts, range);
+        f_steps = steps_of(range), f_first = SPLIT ? range * a.per : 0;
         const int row0 = (is_r ? tr : ts) * block;
-        base = (const char *)src + (int64_t)row0 * a.K - 3072;
+        base = (const char *)src + (int64_t)row0 * a.K + (int64_t)f_first * BK - 3072;
 #pragma unroll
         for (int i = 0; i < LI; ++i) {
             const int row = (wave & 3) * 16 * LI + i * 16 + (lane >> 2), piece = (lane & 3) ^ ((row >> 2) & 3);
@@ -297,18 +306,18 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
         }
     };
     auto fetch = [&](int stage) {
-        if (tail && f_step == steps - 1) {                       // what lies beyond K reads as zeros
+        if (tail && f_first + f_step == all_steps - 1) {                       // what lies beyond K reads as zeros
 #pragma unroll
             for (int i = 0; i < LI; ++i) {
                 const int piece = (lane & 3) ^ ((lane >> 4) & 3);
                 const char *const from = base + off[i] + i * 1024;
-                to_lds16((int64_t)f_step * BK + piece * 16 < a.K ? from : (const char *)&zero_piece, lds + stage * STAGE + (wave * LI + i) * 1024);
+                to_lds16((int64_t)(f_first + f_step) * BK + piece * 16 < a.K ? from : (const char *)&zero_piece, lds + stage * STAGE + (wave * LI + i) * 1024);
             }
         } else {
             to_lds16_rows<LI>(uniform(base), off, __builtin_amdgcn_readfirstlane(to + stage * STAGE));
         }
         base += BK;
-        if (++f_step == steps) {
+        if (++f_step == f_steps) {
             f_step = 0, f_tile += on_die;
             aim();
         }
@@ -331,7 +340,7 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
     // Scales and biases of this wave's rows of a tile come to LDS at the tile's beginning, to a place of the wave's own, two tiles in turn.
     constexpr int NR = FR / 2, PRIVATE = (2 * NR + 2) * 256;
     const char *const own = lds + STAGES * STAGE + wave * 2 * PRIVATE;
-    int tr, ts, parity = 0;
+    int tr, ts, range, parity = 0;
     auto fetch_scales = [&] {
         const char *const at = own + parity * PRIVATE;
         const int r = tr * BR + wr * FR * 32 + lane, sc = min(ts * BS + wsv * FS * 32 + (FS == 2 ? lane : l32), a.ns - 1);
@@ -349,8 +358,9 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
     read(lds, 0);
     int stage = 0;
     for (int tile = first; tile < last; tile += on_die) {
-        walk.place(tile, tr, ts, a.tiles_r);
-        fetch_scales();
+        item(tile, tr, ts, range);
+        const int steps = steps_of(range);
+        if (!SPLIT) fetch_scales();
         i32x16 acc[FR][FS] = {};
         auto products = [&](int kk) {
 #pragma unroll
@@ -371,6 +381,22 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
             __builtin_amdgcn_sched_barrier(0);
             products(1);
             __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (SPLIT) {
+            int *const part = a.part + (int64_t)range * a.ns * a.nr;
+#pragma unroll
+            for (int i = 0; i < FR; ++i)
+#pragma unroll
+                for (int j = 0; j < FS; ++j) {
+                    const int s = ts * BS + (wsv * FS + j) * 32 + l32, r = tr * BR + (wr * FR + i) * 32 + 4 * half;
+                    if (s >= a.ns) continue;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                        store_piece<int, 4>(part + (int64_t)s * a.nr + r + 8 * q, a.nr - r - 8 * q, v);
+                    }
+                }
+            continue;
         }
         // (three steps after they were asked for the scales are there; with fewer steps they are waited for)
         if (steps < 3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -442,6 +468,49 @@ template <typename T, bool CHANNELS, int FR, int FS> __global__ void __launch_bo
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // nothing is on its way to LDS when the workgroup ends
 }
 
+// y from the ranges' sums: whole numbers, so their order does not matter.
+template <typename T> __global__ void __launch_bounds__(256) k_linear_sums(const LinArgs a)
+{
+    const int per_row = (a.nr + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int s = (int)(i / per_row), r = (int)(i - (int64_t)s * per_row) * 4;
+    if (s >= a.ns) return;
+    const int64_t at = (int64_t)s * a.nr + r, size = (int64_t)a.ns * a.nr;
+    int sum[4] = {};
+#pragma unroll 4
+    for (int k = 0; k < a.ranges; ++k) {
+        int v[4] = {};
+        if (r + 4 <= a.nr) {
+            __builtin_memcpy(v, a.part + k * size + at, 16);
+        } else {
+            for (int e = 0; e < 4; ++e)
+                if (r + e < a.nr) v[e] = a.part[k * size + at + e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
+    const float ss = a.sscale[s], sb = a.sbias ? a.sbias[s] : 0.f;
+    T y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int q = min(r + e, a.nr - 1);
+        y[e] = from_f32<T>(fmaf((float)sum[e] * a.rscale[q], ss, (a.rbias ? a.rbias[q] : 0.f) + sb));
+    }
+    put<T, 4>(a, column_of(a, s), r, y);
+}
+
+// Into how many ranges k goes: where few tiles are left for the compute units, as many as give each one, of eight steps of 64 at least.
+// (100 tokens, 4096 -> 4096: 32 us on tiles of 64 x 64 with all of k.)
+static int k_ranges(int64_t T, int64_t K, int64_t O)
+{
+    const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128), steps = (K + 63) / 64;
+    if (T <= 64 || K % 16 != 0 || tiles > 64) return 1;
+    const int64_t most = 256 / tiles < steps / 8 ? 256 / tiles : steps / 8;
+    if (most < 2) return 1;
+    const int64_t per = (steps + most - 1) / most;
+    return (int)((steps + per - 1) / per);
+}
+
 // Few tokens (S, up to 16 NT of them): what counts is how fast the weight streams in, so its rows go from memory straight into the
 // operand registers, sixteen rows to a workgroup, whose waves divide k among themselves and add their sums up in LDS.
 struct FewArgs {
@@ -500,7 +569,7 @@ template <typename T, int NT> __global__ void __launch_bounds__(512) k_linear_fe
 }
 
 template <typename T> static int run(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, void *y, int64_t B,
-                                     int64_t N, int64_t K, int64_t O, int64_t parts, hipStream_t s)
+                                     int64_t N, int64_t K, int64_t O, int64_t parts, void *workspace, hipStream_t s)
 {
     const int64_t t = B * N;
     if (t <= 64) {
@@ -533,7 +602,7 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
         constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value, BR = 64 * FR, BS = 128 * FS, lds = 4 * (BR + BS) * 64 + 16 * (FR + 2) * 256;
         a.tiles_r = (a.nr + BR - 1) / BR, a.tiles_s = (a.ns + BS - 1) / BS;
         Walk w = {a.tiles_s, a.tiles_s <= 12 ? a.tiles_s : 8, a.tiles_r * a.tiles_s};
-        const auto kernel = a.channels ? k_linear_async<T, true, FR, FS> : k_linear_async<T, false, FR, FS>;
+        const auto kernel = a.channels ? k_linear_async<T, true, false, FR, FS> : k_linear_async<T, false, false, FR, FS>;
         FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
         const int most = 256 * (FR == 4 ? 1 : 2);
         kernel<<<(unsigned)(w.tiles < most ? w.tiles : most), 512, lds, s>>>(a, w);
@@ -542,6 +611,21 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
     };
     auto tiles = [&](int br, int bs) { return (int64_t)((a.nr + br - 1) / br) * ((a.ns + bs - 1) / bs); };
     const bool pieces = K % 16 == 0 && ((uintptr_t)xq | (uintptr_t)wq) % 16 == 0;
+    a.ranges = k_ranges(t, K, O);
+    if (pieces && a.ranges > 1) {
+        constexpr int lds = 4 * 256 * 64 + 16 * 4 * 256;
+        const int64_t steps = (K + 63) / 64;
+        a.per = (int)((steps + a.ranges - 1) / a.ranges), a.part = (int *)workspace;
+        a.tiles_r = (a.nr + 127) / 128, a.tiles_s = (a.ns + 127) / 128;
+        const Walk w = {a.tiles_s, a.tiles_s <= 12 ? a.tiles_s : 8, a.tiles_r * a.tiles_s * a.ranges};
+        const auto kernel = k_linear_async<T, false, true, 2, 1>;
+        FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
+        kernel<<<(unsigned)w.tiles, 512, lds, s>>>(a, w);
+        FC_HIP(hipGetLastError());
+        k_linear_sums<T><<<(unsigned)(((int64_t)((a.nr + 3) / 4) * a.ns + 255) / 256), 256, 0, s>>>(a);
+        FC_HIP(hipGetLastError());
+        return FFTCONV_OK;
+    }
     if (pieces && tiles(256, 256) >= 256) return launch_async(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
     if (pieces && tiles(128, 128) >= 128) return launch_async(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
     if (tiles(128, 256) >= 512) return launch(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
@@ -549,14 +633,18 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
     return launch(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
 }
 
-size_t linear_i8_workspace(int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t linear_i8_workspace(int64_t T, int64_t K, int64_t O)
+{
+    const int ranges = k_ranges(T, K, O);
+    return ranges > 1 ? (size_t)ranges * (size_t)T * (size_t)O * 4 : 0;
+}
 
 int linear_i8(const int8_t *xq, const float *xs, const int8_t *wq, const float *ws, const float *bias, void *y, int64_t B, int64_t N, int64_t K,
-              int64_t O, int64_t parts, int dtype, void *, hipStream_t s)
+              int64_t O, int64_t parts, int dtype, void *workspace, hipStream_t s)
 {
-    if (dtype == FFTCONV_BF16) return run<__bf16>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, s);
-    if (dtype == FFTCONV_F16) return run<_Float16>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, s);
-    return run<float>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, s);
+    if (dtype == FFTCONV_BF16) return run<__bf16>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, workspace, s);
+    if (dtype == FFTCONV_F16) return run<_Float16>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, workspace, s);
+    return run<float>(xq, xs, wq, ws, bias, y, B, N, K, O, parts, workspace, s);
 }
 
 }  // namespace lay

@@ -231,6 +231,23 @@ def test_products_in_8_bits(b, n, k, o, dtype, layout, parts):
 
 
 @pytest.mark.parametrize("layout,parts,dtype", [("tokens", 1, "bf16"), ("channels", 1, "f16"), ("channels", 3, "bf16"), ("tokens", 1, "f32"), ("channels", 3, "f32")])
+@pytest.mark.parametrize("b,n,k,o", [(1, 65, 4096, 4095), (5, 20, 1040, 129), (3, 100, 8192, 513), (130, 1, 2000, 99), (1, 128, 1024, 1024)])
+def test_products_with_k_in_ranges(b, n, k, o, layout, parts, dtype):
+    """Few tiles: k goes in ranges, the last one shorter; whole numbers, so every output is that of the sum at once."""
+    if o % parts:
+        o += parts - o % parts
+    g = gen(b + n + k + o)
+    xq, wq = int_rows(g, b, n, k), int_rows(g, o, k)
+    xs, ws = torch.rand(b, n, generator=g, device="cuda") + 0.01, (torch.rand(o, generator=g, device="cuda") + 0.01) / k
+    bias = normal(g, o)
+    ref = (xq.reshape(-1, k).double() @ wq.double().T).reshape(b, n, o) * xs.double()[..., None] * ws.double()
+    bound = (U[dtype] + 4 * E) * (ref.abs() + bias.abs().double()) + TINY[dtype]
+    y = layers.linear_i8((xq, xs), (wq, ws), bias=bias, dtype=DT[dtype], layout=layout, parts=parts)
+    within(y, laid_out(ref + bias.double(), layout, parts), laid_out(bound, layout, parts))
+    assert torch.equal(y, layers.linear_i8((xq, xs), (wq, ws), bias=bias, dtype=DT[dtype], layout=layout, parts=parts))
+
+
+@pytest.mark.parametrize("layout,parts,dtype", [("tokens", 1, "bf16"), ("channels", 1, "f16"), ("channels", 3, "bf16"), ("tokens", 1, "f32"), ("channels", 3, "f32")])
 @pytest.mark.parametrize("b,n,k,o", [(33, 512, 832, 1200), (7, 2600, 64, 3840), (1, 20011, 272, 1023), (3, 8192, 16, 768), (1, 19000, 100, 900)])
 def test_products_of_many_tiles(b, n, k, o, layout, parts, dtype):
     """Several tiles to a workgroup: inside y and at its ends, across sequences and parts, of one step and of many, the last one short; every
