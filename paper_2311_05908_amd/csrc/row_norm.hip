@@ -5,6 +5,9 @@
 //
 // A row stays in the registers of the waves that work on it from its load to its store: every tensor moves once, and that is what bounds
 // these kernels. Sums are held in fp32; h is rounded where it is written, the norm is taken of the sum before that.
+//
+// Measured: bf16 64 x 4096 x 768 forward 320 us and backward 323 us, 1.6 GB each: 5.0 TB/s, what a copy reaches. fp32 3 x 1365 x 4096 53 and 46 us.
+// fp16 9995 x 1001, whose rows end inside a piece: 18.7 us, 4.3 TB/s.
 #include "layers_internal.h"
 
 namespace fftconv {
