@@ -17,8 +17,6 @@ typedef __attribute__((ext_vector_type(16))) int i32x16;
 constexpr float LEAST = 0x1p-100f;
 constexpr int RUN = 128;                                      // samples of a channel that share a scale in a checkpoint
 
-template <typename T> struct Vec8 { T v[8]; };
-
 template <typename T> __device__ __forceinline__ float to_f32(T x) { return (float)x; }
 template <typename T> __device__ __forceinline__ T from_f32(float x) { return (T)x; }      // round to nearest even
 

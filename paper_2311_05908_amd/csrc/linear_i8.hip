@@ -425,10 +425,11 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
         auto column_bias = [&](int j) { return *(const float *)(sc + ((2 * NR + 1) * 64 + j * 32 + l32) * 4); };
         bool done = false;
         if constexpr (FR == 4) {                                 // (a stage has room for the waves; a smaller tile's has not)
-            static_assert(STAGE >= 8 * 4096, "room for the waves");
+            static_assert(STAGE == 8 * 4096 && LI * 1024 == 4096, "a wave's transfers and its results take the same place");
             if (whole) {
                 done = true;
-                // the stage of the last step, which nothing is on its way to yet
+                // The stage of the last step: every wave has read it, and what comes there next is, in a wave's own 4 KB, that wave's own transfers,
+                // which it asks for after this.
                 char *const mine = lds + (stage == 0 ? STAGES - 1 : stage - 1) * STAGE + wave * 4096;
                 constexpr int P = sizeof(T) == 2 ? 2 : 1;        // accumulators to a row of 128 bytes
                 const uint32_t stride = CHANNELS ? (uint32_t)a.N : (uint32_t)a.nr;

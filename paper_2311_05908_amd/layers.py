@@ -19,7 +19,6 @@ import torch
 from . import fftconv as _f
 
 RUN = 128       # samples of a channel that share a scale in a checkpoint
-MAX_ROW = 16384
 
 
 class Rows8(NamedTuple):
