@@ -88,7 +88,7 @@ template <typename T, int W> __device__ __forceinline__ void put(const LinArgs &
 {
     T *const y = (T *)a.y + col;
     if (r + W <= a.nr && (!a.channels || r - quotient(r, a.N, a.by_n) * a.N + W <= a.N)) {
-        __builtin_memcpy(y + row_of(a, r), v, sizeof(v));
+        store_bytes<sizeof(v)>(y + row_of(a, r), v);
     } else {
 #pragma unroll
         for (int e = 0; e < W; ++e)
