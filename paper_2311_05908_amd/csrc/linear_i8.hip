@@ -638,6 +638,8 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     }
+    // The large tile from one for every compute unit on (8192 x 4096 -> 16384: 575 us, and 741 on the small one); below, the small one: with 144 large
+    // ones (4096 x 768 -> 2304) 19.0 us and 20.0, with 128 (2048 x 4096 -> 4096) 46 us and 51.
     if (pieces && tiles(256, 256) >= 256) return launch_async(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
     if (pieces && tiles(128, 128) >= 128) return launch_async(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
     if (tiles(128, 256) >= 512) return launch(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());

@@ -6,8 +6,8 @@
 // A row stays in the registers of the waves that work on it from its load to its store: every tensor moves once, and that is what bounds
 // these kernels. Sums are held in fp32; h is rounded where it is written, the norm is taken of the sum before that.
 //
-// Measured: bf16 64 x 4096 x 768 forward 320 us and backward 323 us, 1.6 GB each: 5.0 TB/s, what a copy reaches. fp32 3 x 1365 x 4096 53 and 46 us.
-// fp16 9995 x 1001, whose rows end inside a piece: 18.7 us, 4.3 TB/s.
+// Measured: bf16 64 x 4096 x 768 forward 300 us and backward 325 us, 1.6 GB each: 5.4 and 5.0 TB/s, what a copy reaches. fp16 9995 x 1001, whose rows
+// end inside a piece: 15 us, 5.4 TB/s; longer tensors of such rows 4 TB/s.
 #include "layers_internal.h"
 
 namespace fftconv {
@@ -211,23 +211,23 @@ __global__ void __launch_bounds__(1024) k_sum_rows(const float *__restrict__ par
     if (slice == 0 && col < D) out[col] = s;
 }
 
-// Which lanes hold a row: one wave for up to 2048 values in 16 bits (1024 in 32), four waves up to 8192 (4096), sixteen above; pieces of
-// 16 bytes, or of 8 where those leave fewer lanes idle (768 values: three pieces of 8 bytes a lane, none idle; two of 16, a quarter idle).
+// Which lanes hold a row: one wave for up to 2048 values in 16 bits (1024 in 32), four waves up to 8192 (4096), sixteen above; pieces of 16 bytes,
+// also where a quarter of the lanes is left idle (768 values: norm and gradients of 64 x 4096 rows 638 us, and 658 with three pieces of 8 bytes
+// and none idle), but not half of them (256 values in 16 bits: 403 us forward for 1.6 GB, 311 in pieces of 8 bytes).
 struct RowShape { int e, ch, wpr; };
 static RowShape row_shape(int64_t D, int dtype)
 {
     const int e = dtype == FFTCONV_F32 ? 4 : 8;
     const int wpr = D <= 64 * e * 4 ? 1 : D <= 256 * e * 4 ? 4 : 16;
-    RowShape s = {e, (int)((D + 64 * wpr * e - 1) / (64 * wpr * e)), wpr};
-    if (e == 8 && D <= 1024 && (D + 255) / 256 * 256 < (D + 511) / 512 * 512) s = {4, (int)((D + 255) / 256), 1};
-    return s;
+    if (e == 8 && D <= 256) return {4, 1, 1};
+    return {e, (int)((D + 64 * wpr * e - 1) / (64 * wpr * e)), wpr};
 }
 
 template <typename F> static int with_row_kernel(int64_t D, int dtype, F f)
 {
     const RowShape s = row_shape(D, dtype);
 #define FC_ROW(TY, E_, CH_, W_) if (s.e == E_ && s.ch == CH_ && s.wpr == W_) return D % E_ == 0 ? f(TY(), std::integral_constant<int, E_>(), std::integral_constant<int, CH_>(), std::integral_constant<int, W_>(), std::true_type()) : f(TY(), std::integral_constant<int, E_>(), std::integral_constant<int, CH_>(), std::integral_constant<int, W_>(), std::false_type());
-#define FC_ROW16(TY) FC_ROW(TY, 4, 1, 1) FC_ROW(TY, 4, 3, 1) FC_ROW(TY, 8, 1, 1) FC_ROW(TY, 8, 2, 1) FC_ROW(TY, 8, 3, 1) FC_ROW(TY, 8, 4, 1) \
+#define FC_ROW16(TY) FC_ROW(TY, 4, 1, 1) FC_ROW(TY, 8, 1, 1) FC_ROW(TY, 8, 2, 1) FC_ROW(TY, 8, 3, 1) FC_ROW(TY, 8, 4, 1) \
         FC_ROW(TY, 8, 2, 4) FC_ROW(TY, 8, 3, 4) FC_ROW(TY, 8, 4, 4) FC_ROW(TY, 8, 2, 16)
     if (dtype == FFTCONV_BF16) {
         FC_ROW16(__bf16)
