@@ -13,6 +13,7 @@
 // dy and q through registers, where it turns dy over, widens q and splits fp32, four waves before the products of a half run and four after
 // them. bf16 8 x 4095, 1024 x 4096: 341 us, where 8 x 4096 takes 318 on the other one.
 #include "async_lds.h"
+#include "layers_index.h"
 
 namespace fftconv {
 namespace lay {
@@ -168,9 +169,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
         const int n0 = j * RUN + h * 64;
         const T *const dy = (const T *)a.dy + (TOKENS ? ((int64_t)b * a.N + n0) * a.O + o0 : ((int64_t)b * a.O + o0) * a.N + n0);
         const int8_t *const q = a.q + ((int64_t)b * a.C + c0) * a.N + n0;
-        // the last piece of a row of dy may reach into the next row, which the last row does not have
-        const bool edge = n0 + 64 > a.N || (TOKENS && a.O % 8 != 0 && n0 + 64 == a.N);
-        if (!edge) {
+        if (whole_half_run(n0, a.N, a.O, TOKENS)) {
 #pragma unroll
             for (int i = 0; i < AV; ++i) {
                 if (TOKENS && threadIdx.x + i * 512 >= BO * 2) continue;
