@@ -63,22 +63,46 @@ template <typename T, typename P> __device__ __forceinline__ void split(const T 
     }
 }
 
-// Two whole numbers of up to eight bits as a pair of 16-bit ones, exactly: of bf16 the upper halves of the fp32 ones.
-__device__ __forceinline__ uint32_t pair_of(float x, float y, __bf16)
-{
-    return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
-}
-__device__ __forceinline__ uint32_t pair_of(float x, float y, _Float16) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y)); }
-template <typename T> __device__ __forceinline__ void widen(uint4 v, uint4 (&o)[2])
-{
-    int8_t q[16];
-    __builtin_memcpy(q, &v, 16);
-    uint32_t w[8];
+// 16 whole numbers of eight bits as 16-bit ones, exactly, or as zeros: a Gate of a run's scale tells which, for where the scale is zero the values stand
+// for zeros, whatever they are. It costs no instruction of the widening. bf16: the upper halves of the fp32 numbers, two put together by a permutation
+// whose selector takes zeros instead. f16: q + 128 in the lowest bits of 1024 is 1024 + 128 + q, of which one multiply-add leaves q, or nothing.
+template <typename T> struct Gate;
+template <> struct Gate<__bf16> {
+    uint32_t pick;
+    __device__ __forceinline__ explicit Gate(float scale = 1.f) : pick(scale == 0.f ? 0x0c0c0c0cu : 0x07060302u) {}
+    __device__ __forceinline__ void widen(uint4 v, uint4 (&o)[2]) const
+    {
+        int8_t q[16];
+        __builtin_memcpy(q, &v, 16);
+        uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = pair_of((float)q[2 * i], (float)q[2 * i + 1], T());
-    o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    o[1] = make_uint4(w[4], w[5], w[6], w[7]);
-}
+        for (int i = 0; i < 8; ++i)
+            w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, (float)q[2 * i + 1]), __builtin_bit_cast(uint32_t, (float)q[2 * i]), pick);
+        o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+};
+template <> struct Gate<_Float16> {
+    typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+    f16x2 by, less;
+    __device__ __forceinline__ explicit Gate(float scale = 1.f)
+    {
+        by = scale == 0.f ? f16x2{0, 0} : f16x2{1, 1};
+        less = scale == 0.f ? f16x2{0, 0} : f16x2{-1152, -1152};
+    }
+    __device__ __forceinline__ void widen(uint4 v, uint4 (&o)[2]) const
+    {
+        const uint32_t q[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t t = __builtin_amdgcn_perm(0x64646464u, q[i / 2], i % 2 ? 0x04030402u : 0x04010400u);
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, t), by, less));
+        }
+        o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+};
 
 // 16 bytes from p, of which the first `left` are wanted and the others read as zero, without reading beyond `end` (the tensor's, which has 16
 // bytes at least): what lies too near the end comes from the last 16 bytes, moved down.
@@ -245,7 +269,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
         for (int i = 0; i < BV; ++i) {
             const int p = threadIdx.x + i * 512;
             uint4 t[2];
-            widen<P>(db[i], t);
+            Gate<P>().widen(db[i], t);
 #pragma unroll
             for (int h = 0; h < 2; ++h) *(uint4 *)(base + NP * BO * 128 + place(p >> 2, (p & 3) * 2 + h)) = t[h];
         }
@@ -277,7 +301,17 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
     do {
         f32x16 acc[FO][FC] = {};
         float unit[FC] = {}, top[FC] = {};         // the scale that the sums are in units of, and the largest so far
+        uint32_t zeros = 0;                        // bit j: the run's scale is zero, and so is what its q stands for, whatever that is
         auto products = [&](int buf) {
+            if (__builtin_amdgcn_ballot_w64(zeros != 0) != 0) {        // every lane clears what it reads below (two waves the same places)
+#pragma unroll
+                for (int j = 0; j < FC; ++j) {
+                    if (zeros >> j & 1) {
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) *(uint4 *)(lds + buf * STAGE + (rc ^ (kk << 5)) + j * 32 * 128) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+            }
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
                 const char *const pc = lds + buf * STAGE + (rc ^ (kk << 5)), *const po = lds + buf * STAGE + (ro ^ (kk << 5));
@@ -301,9 +335,11 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 #pragma unroll
             for (int j = 0; j < FC; ++j) small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
             if (__builtin_amdgcn_ballot_w64(small) != 0) break;
+            zeros = 0;
 #pragma unroll
             for (int j = 0; j < FC; ++j) {
                 // a run of zeros keeps the units; so do the first sums
+                zeros |= (s[j] == 0.f ? 1u : 0u) << j;
                 const float f = s[j] == 0.f || unit[j] == 0.f ? 1.f : unit[j] / s[j];
                 unit[j] = s[j] == 0.f ? unit[j] : s[j];
                 top[j] = fmaxf(top[j], unit[j]);
@@ -457,17 +493,21 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 #pragma unroll
         for (int j = 0; j < FC; ++j) raw[j] = *(const uint4 *)(base + (rq ^ (u << 5)) + j * 32 * 64);
     };
+    float s[FC] = {};                                            // this lane's scales of the run whose q is widened next
+    Gate<T> gate[FC];
     auto widen_q = [&](int u) {
 #pragma unroll
-        for (int j = 0; j < FC; ++j) widen<T>(raw[j], fc[u][j]);
+        for (int j = 0; j < FC; ++j) gate[j].widen(raw[j], fc[u][j]);
     };
     float *const part = a.part + (int64_t)range * a.O * a.C;
     bool aside = false;
     int blk = first, stage = 0;
-    float s[FC] = {};
     auto read_scales = [&](const char *base) {
 #pragma unroll
-        for (int j = 0; j < FC; ++j) s[j] = *(const float *)(base + S_AT + wave * 256 + (j * 32 + l32) * 4);
+        for (int j = 0; j < FC; ++j) {
+            s[j] = *(const float *)(base + S_AT + wave * 256 + (j * 32 + l32) * 4);
+            gate[j] = Gate<T>(s[j]);
+        }
     };
     if (blk < last) {
         fetch(0, 0);
