@@ -353,16 +353,18 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
     int tr, ts, range, parity = 0;
     auto fetch_scales = [&] {
         const char *const at = own + parity * PRIVATE;
-        const int r = tr * BR + wr * FR * 32 + lane, sc = min(ts * BS + wsv * FS * 32 + (FS == 2 ? lane : l32), a.ns - 1);
+        // (from the tile's first row on: a tensor may have more rows than 32 bits count bytes)
+        const int r0 = tr * BR, s0 = ts * BS, r = r0 + wr * FR * 32 + lane;
+        const uint32_t so = (uint32_t)(min(s0 + wsv * FS * 32 + (FS == 2 ? lane : l32), a.ns - 1) - s0) * 4u;
         const char *const zero = (const char *)&zero_piece;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const uint32_t o = (uint32_t)min(r + i * 64, a.nr - 1) * 4u;
-            to_lds4(uniform((const char *)a.rscale), o, at + i * 256);
-            if (!CHANNELS) to_lds4(uniform(a.rbias ? (const char *)a.rbias : zero), a.rbias ? o : 0, at + (NR + i) * 256);
+            const uint32_t o = (uint32_t)(min(r + i * 64, a.nr - 1) - r0) * 4u;
+            to_lds4(uniform((const char *)(a.rscale + r0)), o, at + i * 256);
+            if (!CHANNELS) to_lds4(uniform(a.rbias ? (const char *)(a.rbias + r0) : zero), a.rbias ? o : 0, at + (NR + i) * 256);
         }
-        to_lds4(uniform((const char *)a.sscale), (uint32_t)sc * 4u, at + 2 * NR * 256);
-        if (CHANNELS) to_lds4(uniform(a.sbias ? (const char *)a.sbias : zero), a.sbias ? (uint32_t)sc * 4u : 0, at + (2 * NR + 1) * 256);
+        to_lds4(uniform((const char *)(a.sscale + s0)), so, at + 2 * NR * 256);
+        if (CHANNELS) to_lds4(uniform(a.sbias ? (const char *)(a.sbias + s0) : zero), a.sbias ? so : 0, at + (2 * NR + 1) * 256);
     };
     FC_ARRIVED(2 * LI);
     read(lds, 0);
