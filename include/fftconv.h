@@ -270,7 +270,7 @@ int fftconv_quantize_rows(const void *x, int64_t ldx, int8_t *q, float *scale, i
 
 /* Projection in 8 bits: for the tokens t = (b, n) of B sequences of N samples
  *     y[t, o] = (sum over k of x[t, k] w[o, k]) x_scale[t] w_scale[o] + bias[o],
- * the sum in 32-bit integers, exact.  x: (B, N, K), w: (O, K), contiguous; bias: O fp32 or NULL; 1 <= K <= 131071; B N and O below 2^31.
+ * the sum in 32-bit integers, exact.  x: (B, N, K), w: (O, K), contiguous; bias: O fp32 or NULL; 1 <= K <= 131071; B N and O up to 2^31 - 512, B N O up to 2^42.
  *   parts = 0: y is (B, N, O), token by token.  parts >= 1, a divisor of O: y is (parts, B, O / parts, N), channel by channel, what the
  *   convolutions take: with parts = 3, u, w and v of fftconv_forward_gated lie one after the other.  dtype: of y.
  *   workspace: fftconv_workspace_bytes_linear_i8 bytes (may be NULL when that is 0). */

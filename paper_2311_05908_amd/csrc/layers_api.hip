@@ -6,6 +6,8 @@ using namespace fftconv;
 namespace {
 
 constexpr int64_t MOST = ((int64_t)1 << 31) - 1;
+constexpr int64_t MOST_ROWS = MOST + 1 - 512;      // of a projection's operands: the end of the last tile, and a store's beyond it, fit 32 bits
+constexpr int64_t MOST_OUT = (int64_t)1 << 42;     // values of a projection's result, so that its tiles are a number of 32 bits
 constexpr int64_t MOST_K = 131071;                 // sums of so many products of 8-bit numbers fit 32 bits
 
 int bad(const char *who, const char *what)
@@ -48,8 +50,13 @@ int check_acts(const char *who, int64_t B, int64_t C, int64_t N, int dtype)
 int check_linear(const char *who, int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype)
 {
     if (!known(dtype)) return bad(who, "unknown dtype");
-    if (B < 0 || N < 1 || K < 1 || O < 1 || times(B, N) < 0 || O > MOST) return bad(who, "B >= 0, N, K, O >= 1 are wanted, B N and O below 2^31");
+    if (B < 0 || N < 1 || K < 1 || O < 1 || times(B, N, MOST_ROWS) < 0 || O > MOST_ROWS)
+        return bad(who, "B >= 0, N, K, O >= 1 are wanted, B N and O up to 2^31 - 512");
     if (parts < 0 || (parts > 0 && O % parts != 0)) return bad(who, "parts has to divide O");
+    if (times(B * N, O, MOST_OUT) < 0) {
+        set_error("%s: B N O=%lld x %lld values of y: up to 2^42 are supported", who, (long long)(B * N), (long long)O);
+        return FFTCONV_EUNSUPPORTED;
+    }
     if (K > MOST_K) {
         set_error("%s: sums of K=%lld products may leave 32 bits: up to %lld are supported", who, (long long)K, (long long)MOST_K);
         return FFTCONV_EUNSUPPORTED;

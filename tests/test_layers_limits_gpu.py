@@ -62,3 +62,17 @@ def test_products_of_more_rows_than_32_bits_count_bytes_of_scales(layout, o):
     check_places(y, xq, xs, wq, ws, layout, [(0, j) for j in (0, 1 << 15, 1 << 29, (1 << 30) - 1, 1 << 30, (1 << 30) + 300, (1 << 30) + 2049, n - 1)])
     del xq, xs, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("b,n", [(512, 4194303), (331, 6487863)])
+def test_products_of_nearly_2_31_rows(b, n):
+    """2^31 - 512 tokens, the most that are taken, and 2^31 - 995, which end inside a tile; several sequences, whose ends lie inside tiles."""
+    g = gen(62)
+    k = 16
+    xq = torch.randint(-128, 128, (b, n, k), generator=g, device="cuda", dtype=torch.int8)
+    wq, ws = int_rows(g, 1, k), torch.rand(1, generator=g, device="cuda") + 0.1
+    xs = torch.rand(b, n, generator=g, device="cuda") + 0.1
+    y = layers.linear_i8((xq, xs), (wq, ws), layout="channels")
+    check_places(y, xq, xs, wq, ws, "channels", [(i, j) for i in (0, 1, b // 2, b // 2 + 1, b - 1) for j in (0, n // 3, n - 1)])
+    del xq, xs, y
+    torch.cuda.empty_cache()
