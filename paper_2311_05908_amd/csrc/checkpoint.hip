@@ -5,6 +5,7 @@
 //
 // Runs lie along the samples because that is the direction every gradient here sums over (a filter's, a projection's): within a run
 // the scale comes out of the sum. Bound by the bytes moved: bf16 64 x 768 x 4096 packed in 129 us (4.7 TB/s), read back as a product in 129 us (6.2).
+#include "layers_index.h"
 #include "layers_internal.h"
 
 namespace fftconv {
@@ -25,10 +26,10 @@ template <typename T, bool WHOLE> __device__ __forceinline__ bool run_at(int64_t
 }
 
 template <typename T, bool WHOLE> __global__ void __launch_bounds__(256) k_pack(const T *__restrict__ x, int8_t *__restrict__ q, float *__restrict__ scale,
-                                                                                int64_t total, int64_t runs, int64_t N)
+                                                                                int64_t first, int64_t total, int64_t runs, int64_t N)
 {
     constexpr int R = 2;
-    const int64_t i0 = (int64_t)blockIdx.x * 16 * R + (threadIdx.x >> 4);
+    const int64_t i0 = (first + blockIdx.x) * (16 * R) + (threadIdx.x >> 4);
     float v[R][8];
     int64_t at[R], left[R];
     bool there[R];
@@ -55,13 +56,13 @@ template <typename T, bool WHOLE> __global__ void __launch_bounds__(256) k_pack(
 // exchanges, and over the four waves by way of LDS. bf16 64 x 4096 x 768: 189 us, 3.2 TB/s (199 with LDS's atomic maximum): more than the bytes,
 // for the steps of a workgroup follow each other.
 template <typename T> __global__ void __launch_bounds__(256) k_pack_tokens(const T *__restrict__ x, int8_t *__restrict__ q, float *__restrict__ scale,
-                                                                            int64_t C, int64_t N, uint32_t runs, uint32_t cgroups)
+                                                                            int64_t C, int64_t N, uint32_t runs, uint32_t cgroups, uint32_t first)
 {
     __shared__ __align__(16) uint32_t tops[4][64];
     __shared__ uint32_t tile[64][RUN / 4 + 1];                 // [channel][samples, four to a word]
     const int piece8 = threadIdx.x & 7, lane = threadIdx.x & 63;
-    const uint32_t at = blockIdx.x / cgroups;              // (numbers of 32 bits: a division of 64 takes a tenth of a workgroup's time)
-    const int64_t cg = blockIdx.x - at * cgroups, j = at % runs, b = at / runs;
+    const uint32_t i = first + blockIdx.x, at = i / cgroups;      // (numbers of 32 bits: a division of 64 takes a tenth of a workgroup's time)
+    const int64_t cg = i - at * cgroups, j = at % runs, b = at / runs;
     const int64_t c0 = cg * 64 + piece8 * 8, n0 = j * RUN + (threadIdx.x >> 3) * 4;
     float v[4][8];
 #pragma unroll
@@ -108,11 +109,11 @@ template <typename T> __global__ void __launch_bounds__(256) k_pack_tokens(const
 
 template <typename T, bool WHOLE> __global__ void __launch_bounds__(256) k_unpack(const int8_t *__restrict__ q, const float *__restrict__ scale,
                                                                                   const int8_t *__restrict__ gq, const float *__restrict__ gscale,
-                                                                                  const T *__restrict__ gate, T *__restrict__ x, int64_t total,
-                                                                                  int64_t runs, int64_t N)
+                                                                                  const T *__restrict__ gate, T *__restrict__ x, int64_t first,
+                                                                                  int64_t total, int64_t runs, int64_t N)
 {
     constexpr int R = 2;
-    const int64_t i0 = (int64_t)blockIdx.x * 16 * R + (threadIdx.x >> 4);
+    const int64_t i0 = (first + blockIdx.x) * (16 * R) + (threadIdx.x >> 4);
     float v[R][8], g[R][8], s[R], gs[R];
     int64_t at[R], left[R];
 #pragma unroll
@@ -156,15 +157,19 @@ int act_pack(const void *x, int8_t *q, float *scale, int64_t B, int64_t C, int64
                 set_error("fftconv_act_pack: %lld tiles of 64 channels x 128 samples: up to 2^31 - 1 are supported", (long long)total);
                 return FFTCONV_EUNSUPPORTED;
             }
-            k_pack_tokens<T><<<(unsigned)total, 256, 0, s>>>((const T *)x, q, scale, C, N, (uint32_t)runs, (uint32_t)cg);
-        } else {
-            const int64_t total = B * C * runs;
-            const unsigned g = (unsigned)((total + 31) / 32);
-            if (N % RUN == 0) k_pack<T, true><<<g, 256, 0, s>>>((const T *)x, q, scale, total, runs, N);
-            else k_pack<T, false><<<g, 256, 0, s>>>((const T *)x, q, scale, total, runs, N);
+            return in_pieces(total, 256, [&](int64_t first, unsigned g) -> int {
+                k_pack_tokens<T><<<g, 256, 0, s>>>((const T *)x, q, scale, C, N, (uint32_t)runs, (uint32_t)cg, (uint32_t)first);
+                FC_HIP(hipGetLastError());
+                return FFTCONV_OK;
+            });
         }
-        FC_HIP(hipGetLastError());
-        return FFTCONV_OK;
+        const int64_t total = B * C * runs;
+        return in_pieces((total + 31) / 32, 256, [&](int64_t first, unsigned g) -> int {
+            if (N % RUN == 0) k_pack<T, true><<<g, 256, 0, s>>>((const T *)x, q, scale, first, total, runs, N);
+            else k_pack<T, false><<<g, 256, 0, s>>>((const T *)x, q, scale, first, total, runs, N);
+            FC_HIP(hipGetLastError());
+            return FFTCONV_OK;
+        });
     });
 }
 
@@ -174,11 +179,12 @@ int act_unpack(const int8_t *q, const float *scale, const int8_t *gq, const floa
     const int64_t runs = (N + RUN - 1) / RUN, total = B * C * runs;
     return with_type(dtype, [&](auto t) -> int {
         using T = decltype(t);
-        const unsigned g = (unsigned)((total + 31) / 32);
-        if (N % RUN == 0) k_unpack<T, true><<<g, 256, 0, s>>>(q, scale, gq, gscale, (const T *)gate, (T *)x, total, runs, N);
-        else k_unpack<T, false><<<g, 256, 0, s>>>(q, scale, gq, gscale, (const T *)gate, (T *)x, total, runs, N);
-        FC_HIP(hipGetLastError());
-        return FFTCONV_OK;
+        return in_pieces((total + 31) / 32, 256, [&](int64_t first, unsigned g) -> int {
+            if (N % RUN == 0) k_unpack<T, true><<<g, 256, 0, s>>>(q, scale, gq, gscale, (const T *)gate, (T *)x, first, total, runs, N);
+            else k_unpack<T, false><<<g, 256, 0, s>>>(q, scale, gq, gscale, (const T *)gate, (T *)x, first, total, runs, N);
+            FC_HIP(hipGetLastError());
+            return FFTCONV_OK;
+        });
     });
 }
 

@@ -16,5 +16,15 @@ __host__ __device__ inline bool whole_half_run(int64_t n0, int64_t N, int64_t O,
     return after >= 0 && (!tokens || after * O >= (O + 7) / 8 * 8 - O);
 }
 
+// A launch holds less than 2^32 threads (a longer one is cut short without an error): more workgroups go out in pieces, f(the first one's number,
+// how many), until one of them returns a code other than 0.
+template <typename F> inline int in_pieces(int64_t groups, int threads, F f)
+{
+    const int64_t most = (((int64_t)1 << 32) - 1) / threads;
+    for (int64_t first = 0; first < groups; first += most)
+        if (const int rc = f(first, (unsigned)(groups - first < most ? groups - first : most))) return rc;
+    return 0;
+}
+
 }  // namespace lay
 }  // namespace fftconv

@@ -48,3 +48,24 @@ def test_reads_of_a_gradient_of_few_channels(tmp_path, channels, after):
     """The last piece of 8 reaches over several samples: not read whole with so few behind it."""
     ask = compiled(tmp_path, 'long long n0, n, o; while (std::scanf("%lld %lld %lld", &n0, &n, &o) == 3) std::printf("%d\\n", (int)whole_half_run(n0, n, o, true));')
     assert ask([(0, 64 + after, channels), (64, 128 + after, channels), (0, 64 + after + 1, channels)]) == [(0,), (0,), (1,)]
+
+
+@pytest.mark.parametrize("threads", [64, 256, 512])
+def test_launches_of_less_than_2_32_threads(tmp_path, threads):
+    """Every workgroup in one launch, in order, none with 2^32 threads; a launch that fails is the last."""
+    ask = compiled(tmp_path, """
+    long long n, stop;
+    while (std::scanf("%%lld %%lld", &n, &stop) == 2) {
+        long long next = 0, calls = 0;
+        const int rc = in_pieces(n, %d, [&](int64_t first, unsigned g) -> int {
+            if (first != next || g < 1 || (long long)g * %d >= 1LL << 32) return -99;
+            next = first + g;
+            return ++calls == stop ? -5 : 0;
+        });
+        std::printf("%%d %%lld %%lld\\n", rc, calls, next);
+    }""" % (threads, threads))
+    most = ((1 << 32) - 1) // threads
+    for n in (1, 2, most - 1, most, most + 1, 2 * most, 2 * most + 1, (1 << 35) // 32, (1 << 31) - 1):
+        calls = -(-n // most)
+        assert ask([(n, 0), (n, 1)]) == [(0, calls, n), (-5, 1, min(n, most))]
+    assert ask([(0, 0)]) == [(0, 0, 0)]

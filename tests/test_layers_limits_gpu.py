@@ -76,3 +76,17 @@ def test_products_of_nearly_2_31_rows(b, n):
     check_places(y, xq, xs, wq, ws, "channels", [(i, j) for i in (0, 1, b // 2, b // 2 + 1, b - 1) for j in (0, n // 3, n - 1)])
     del xq, xs, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("layout,shape", [("channels", ((1 << 20) + 3, 513, 1)), ("tokens", ((1 << 24) + 5, 1, 64)), ("tokens", ((1 << 18) + 1, 1, 4097))])
+def test_checkpoints_of_more_runs_than_a_launch_has_threads_for(layout, shape):
+    """Single samples, a run each: 2^29 runs, and 2^24 tiles, are 2^32 threads and more. 127 steps of a value's own scale are the value, to bf16."""
+    x = torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_(generator=gen(71)).abs_().clamp_(min=2.0 ** -20)
+    x[::2] *= -1
+    p = layers.act_pack(x, layout=layout)
+    assert p.q.shape[2] == 1 and p.scale.shape == p.q.shape
+    assert int(p.q.min()) == -127 and int(p.q.max()) == 127 and int((p.q == 0).sum()) == 0 and float(p.scale.min()) > 0
+    back = layers.act_unpack(p)
+    assert torch.equal(back.reshape(shape[0], -1), x.reshape(shape[0], -1))
+    p = None
+    torch.cuda.empty_cache()
