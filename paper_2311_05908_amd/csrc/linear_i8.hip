@@ -10,6 +10,7 @@
 // where there is one for every compute unit, else of 128 x 128, with k in ranges where there are few of those; else k_linear, which takes any k
 // at any alignment (4097 x 4097 -> 4097: 0.69 POP/s, where 4096 x 4096 -> 4096 makes 1.96).
 #include "async_lds.h"
+#include "layers_index.h"
 
 namespace fftconv {
 namespace lay {
@@ -26,6 +27,7 @@ struct LinArgs {
     uint32_t by_n, by_part;       // 2^32 over these, rounded up
     int64_t B;
     int tiles_r, tiles_s;
+    int first;                    // tile of a launch's first workgroup (k_linear)
     int ranges, per;              // of k, whose sums of a tile are added up by a second kernel (1: all of k); steps of one
     int *part;                    // (ranges, ns, nr)
 };
@@ -188,7 +190,7 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) 
     __shared__ __align__(16) char lds[2 * G::STAGE];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int wr = wave >> 1, wsv = wave & 1;
-    const int tr = blockIdx.x / a.tiles_s, ts = blockIdx.x % a.tiles_s;
+    const int tile = a.first + (int)blockIdx.x, tr = tile / a.tiles_s, ts = tile % a.tiles_s;
     const int r0 = tr * G::BR, s0 = ts * G::BS;
     const int8_t *src[PIECES];
     int dst[PIECES];
@@ -533,13 +535,14 @@ struct FewArgs {
     void *y;
     int64_t K, B;
     int T, O, channels, N, per_part;
+    int first;                    // output of a launch's first workgroup
 };
 
 template <typename T, int NT> __global__ void __launch_bounds__(512) k_linear_few(const FewArgs a)
 {
     __shared__ i32x4 sums[8][NT][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
-    const int o0 = blockIdx.x * 16;
+    const int o0 = a.first + (int)blockIdx.x * 16;
     const int8_t *const w = a.w + (int64_t)min(o0 + l16, a.O - 1) * a.K;
     const int8_t *x[NT];
 #pragma unroll
@@ -587,13 +590,15 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
 {
     const int64_t t = B * N;
     if (t <= 64) {
-        const FewArgs a = {xq, wq, xs, ws, bias, y, K, B, (int)t, (int)O, parts > 0, (int)N, (int)(parts ? O / parts : O)};
-        const unsigned g = (unsigned)((O + 15) / 16);
-        if (t <= 16) k_linear_few<T, 1><<<g, 512, 0, s>>>(a);
-        else if (t <= 32) k_linear_few<T, 2><<<g, 512, 0, s>>>(a);
-        else k_linear_few<T, 4><<<g, 512, 0, s>>>(a);
-        FC_HIP(hipGetLastError());
-        return FFTCONV_OK;
+        FewArgs a = {xq, wq, xs, ws, bias, y, K, B, (int)t, (int)O, parts > 0, (int)N, (int)(parts ? O / parts : O), 0};
+        return in_pieces((O + 15) / 16, 512, [&](int64_t first, unsigned g) -> int {
+            a.first = (int)(first * 16);
+            if (t <= 16) k_linear_few<T, 1><<<g, 512, 0, s>>>(a);
+            else if (t <= 32) k_linear_few<T, 2><<<g, 512, 0, s>>>(a);
+            else k_linear_few<T, 4><<<g, 512, 0, s>>>(a);
+            FC_HIP(hipGetLastError());
+            return FFTCONV_OK;
+        });
     }
     LinArgs a = {};
     a.channels = parts > 0;
@@ -608,9 +613,12 @@ template <typename T> static int run(const int8_t *xq, const float *xs, const in
         constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value;
         using G = Tile<FR, FS>;
         a.tiles_r = (a.nr + G::BR - 1) / G::BR, a.tiles_s = (a.ns + G::BS - 1) / G::BS;
-        k_linear<T, FR, FS><<<(unsigned)((int64_t)a.tiles_r * a.tiles_s), 256, 0, s>>>(a);
-        FC_HIP(hipGetLastError());
-        return FFTCONV_OK;
+        return in_pieces((int64_t)a.tiles_r * a.tiles_s, 256, [&](int64_t first, unsigned g) -> int {
+            a.first = (int)first;
+            k_linear<T, FR, FS><<<g, 256, 0, s>>>(a);
+            FC_HIP(hipGetLastError());
+            return FFTCONV_OK;
+        });
     };
     auto launch_async = [&](auto fr, auto fs) -> int {
         constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value, BR = 64 * FR, BS = 128 * FS, lds = 4 * (BR + BS) * 64 + 16 * (FR + 2) * 256;

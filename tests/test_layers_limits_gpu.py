@@ -90,3 +90,32 @@ def test_checkpoints_of_more_runs_than_a_launch_has_threads_for(layout, shape):
     assert torch.equal(back.reshape(shape[0], -1), x.reshape(shape[0], -1))
     p = None
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("t,layout", [(1, "tokens"), (3, "channels"), (20, "tokens")])
+def test_products_of_few_tokens_into_more_channels_than_a_launch_has_threads_for(t, layout):
+    """From 2^27 outputs on, 512 threads for sixteen of them, a launch has 2^32 threads; k = 1."""
+    g = gen(72)
+    o = (1 << 27) + 77
+    xq, wq = int_rows(g, 1, t, 1), int_rows(g, o, 1)
+    xs, ws = torch.rand(1, t, generator=g, device="cuda") + 0.1, torch.rand(o, generator=g, device="cuda") + 0.1
+    y = layers.linear_i8((xq, xs), (wq, ws), layout=layout)
+    for i in range(t):
+        ref = wq[:, 0].float() * float(xq[0, i, 0]) * ws * xs[0, i]
+        got = (y[0, i] if layout == "tokens" else y[0, :, i]).float()
+        assert bool(((got - ref).abs() <= (U["bf16"] + 8 * E) * ref.abs()).all()), i
+    del y
+    torch.cuda.empty_cache()
+
+
+def test_products_of_nearly_2_31_rows_of_no_sixteens():
+    """2^31 - 512 tokens with k = 3: 2^24 - 4 tiles of 128, a launch of nearly 2^32 threads."""
+    g = gen(73)
+    b, n, k = 512, 4194303, 3
+    xq = torch.randint(-128, 128, (b, n, k), generator=g, device="cuda", dtype=torch.int8)
+    wq, ws = int_rows(g, 1, k), torch.rand(1, generator=g, device="cuda") + 0.1
+    xs = torch.rand(b, n, generator=g, device="cuda") + 0.1
+    y = layers.linear_i8((xq, xs), (wq, ws), layout="channels")
+    check_places(y, xq, xs, wq, ws, "channels", [(i, j) for i in (0, 1, 255, 256, 257, 510, 511) for j in (0, n // 3, n - 1)])
+    del xq, xs, y
+    torch.cuda.empty_cache()
