@@ -285,7 +285,7 @@ int fftconv_linear_i8(const int8_t *x, const float *x_scale, const int8_t *w, co
  *   (what the gradients of a gated convolution take: u . w for fftconv_backward_filter).  gate_q with gate_scale, or gate, or none.
  * fftconv_linear_grad_weight: the gradient of a projection's weight from its kept input,
  *     dw[o, c] = sum over b, n of dy[b, n, o] q[b, c, n] scale[b, c, n / 128].
- *   dy: (B, N, O) with tokens = 1, else (B, O, N).  dw: (O, C), fp32 or dtype (dtype_dw).  N, O and C up to 2^22.
+ *   dy: (B, N, O) with tokens = 1, else (B, O, N).  dw: (O, C), fp32 or dtype (dtype_dw).  N, O and C up to 2^22, O C up to 2^36.
  *   A run whose scale is zero stands for zeros, whatever its q.
  *   Products are exact (8-bit values times dy), sums in fp32.  workspace: fftconv_workspace_bytes_linear_grad_weight bytes. */
 int fftconv_act_pack(const void *x, int8_t *q, float *scale, int64_t B, int64_t C, int64_t N, int tokens, int dtype, void *stream);

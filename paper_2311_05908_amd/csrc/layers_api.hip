@@ -8,6 +8,7 @@ namespace {
 constexpr int64_t MOST = ((int64_t)1 << 31) - 1;
 constexpr int64_t MOST_ROWS = MOST + 1 - 512;      // of a projection's operands: the end of the last tile, and a store's beyond it, fit 32 bits
 constexpr int64_t MOST_OUT = (int64_t)1 << 42;     // values of a projection's result, so that its tiles are a number of 32 bits
+constexpr int64_t MOST_DW = (int64_t)1 << 36;      // values of a weight's gradient
 constexpr int64_t MOST_K = 131071;                 // sums of so many products of 8-bit numbers fit 32 bits
 
 int bad(const char *who, const char *what)
@@ -71,6 +72,10 @@ int check_weight(const char *who, int64_t B, int64_t N, int64_t O, int64_t C, in
         return bad(who, "B >= 0, N, O, C >= 1 are wanted, N, O, C and B ceil(N / 128) below 2^31");
     if (N > ((int64_t)1 << 22) || O > ((int64_t)1 << 22) || C > ((int64_t)1 << 22)) {        // (distances inside a tile are 32-bit numbers)
         set_error("%s: sequences of %lld samples, %lld x %lld channels: up to 2^22 are supported", who, (long long)N, (long long)O, (long long)C);
+        return FFTCONV_EUNSUPPORTED;
+    }
+    if (O * C > MOST_DW) {                             // (tiles of 512 threads: a launch has less than 2^32)
+        set_error("%s: %lld x %lld values of dw: up to 2^36 are supported", who, (long long)O, (long long)C);
         return FFTCONV_EUNSUPPORTED;
     }
     return FFTCONV_OK;

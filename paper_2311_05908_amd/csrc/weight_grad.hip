@@ -584,9 +584,9 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 }
 
 // Tensors of less than the 16 bytes that a load of the kernel above takes (a handful of values): a thread for each of dw's.
-template <typename T, bool TOKENS, typename DW> __global__ void __launch_bounds__(64) k_weight_tiny(const WeightArgs a)
+template <typename T, bool TOKENS, typename DW> __global__ void __launch_bounds__(64) k_weight_tiny(const WeightArgs a, int64_t first)
 {
-    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    const int64_t i = (first + blockIdx.x) * 64 + threadIdx.x;
     if (i >= (int64_t)a.O * a.C) return;
     const int64_t o = i / a.C, c = i - o * a.C;
     float sum = 0.f;
@@ -672,11 +672,12 @@ template <typename T, typename DW> static int run(const WeightShape &w, const We
     using Y = std::true_type;
     using No = std::false_type;
     if ((int64_t)a.sequences * a.N * a.O * (int64_t)sizeof(T) < 16 || (int64_t)a.sequences * a.N * a.C < 16) {
-        const unsigned g = (unsigned)(((int64_t)a.O * a.C + 63) / 64);
-        if (tokens) k_weight_tiny<T, true, DW><<<g, 64, 0, s>>>(a);
-        else k_weight_tiny<T, false, DW><<<g, 64, 0, s>>>(a);
-        FC_HIP(hipGetLastError());
-        return FFTCONV_OK;
+        return in_pieces(((int64_t)a.O * a.C + 63) / 64, 64, [&](int64_t at, unsigned g) -> int {
+            if (tokens) k_weight_tiny<T, true, DW><<<g, 64, 0, s>>>(a, at);
+            else k_weight_tiny<T, false, DW><<<g, 64, 0, s>>>(a, at);
+            FC_HIP(hipGetLastError());
+            return FFTCONV_OK;
+        });
     }
     if constexpr (sizeof(T) == 2) {
         if (w.fo == 4) {

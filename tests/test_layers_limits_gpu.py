@@ -3,7 +3,7 @@ test_layers_gpu.py."""
 import pytest
 import torch
 
-from paper_2311_05908_amd import layers
+from paper_2311_05908_amd import fftconv, layers
 from test_layers_gpu import DT, E, RUN, U, gen, int_rows, normal, runs8, weight_check, within
 
 pytestmark = pytest.mark.gpu
@@ -118,4 +118,18 @@ def test_products_of_nearly_2_31_rows_of_no_sixteens():
     y = layers.linear_i8((xq, xs), (wq, ws), layout="channels")
     check_places(y, xq, xs, wq, ws, "channels", [(i, j) for i in (0, 1, 255, 256, 257, 510, 511) for j in (0, n // 3, n - 1)])
     del xq, xs, y
+    torch.cuda.empty_cache()
+
+
+def test_weight_gradient_of_no_sequences_into_more_values_than_a_launch_has_threads_for():
+    """2^32 zeros, a thread for each, through the C ABI (the binding makes them itself)."""
+    lib = fftconv.load()
+    o, c = 1 << 16, (1 << 16) + 1
+    dw = torch.ones(o, c, device="cuda")
+    need = lib.fftconv_workspace_bytes_linear_grad_weight(0, 5, o, c, 1, 0)
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    some = torch.zeros(16, device="cuda").data_ptr()
+    assert lib.fftconv_linear_grad_weight(some, some, some, dw.data_ptr(), 0, 5, o, c, 1, 0, 0, work.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    assert not bool(dw.any())
+    del dw, work
     torch.cuda.empty_cache()
