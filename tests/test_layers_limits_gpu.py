@@ -133,3 +133,18 @@ def test_weight_gradient_of_no_sequences_into_more_values_than_a_launch_has_thre
     assert not bool(dw.any())
     del dw, work
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_norm_of_a_slice_goes_back_without_a_residual(dtype):
+    """h is what the backward pass takes also where x is a slice of wider rows and there is no residual."""
+    g = gen(31)
+    wide, dy = normal(g, 3, 11, 900, dtype=DT[dtype]), normal(g, 3, 11, 700, dtype=DT[dtype])
+    w = 1 + 0.1 * normal(g, 700)
+    x = wide[..., 101:801]
+    for norm in (layers.rms_norm, layers.rms_norm_i8):
+        y, h, rstd = norm(x, w)
+        yc, hc, rc = norm(x.contiguous(), w)
+        assert torch.equal(h, x) and torch.equal(rstd, rc)
+        assert all(torch.equal(a, b) for a, b in zip(y, yc))
+        assert all(torch.equal(a, b) for a, b in zip(layers.rms_norm_backward(dy, h, w, rstd), layers.rms_norm_backward(dy, hc, w, rc)))
