@@ -255,7 +255,8 @@ int fftconv_backward_filter(const fftconv_plan *plan, const void *u, const void 
  *     h = x + residual,  y = h / sqrt(mean(h^2) + eps) * weight.
  *   residual may be NULL (h = x).  ldx, ldr: distance between rows of x and of the residual in elements, >= D.  weight: D fp32.  y, h:
  *   contiguous; h (the residual stream for the next layer, rounded to dtype; the norm is taken of the sum before that) and rstd (T
- *   fp32, for the backward pass) may be NULL.  scale: NULL, and y is in dtype; or T fp32, and y is in 8 bits with a scale for each row.
+ *   fp32, for the backward pass) may be NULL.  Rows may hold any finite numbers: where their squares leave fp32 the row is taken in
+ *   units of its own (rstd is then what fp32 holds of it, infinity for rows below 3e-39 with eps = 0).  scale: NULL, and y is in dtype; or T fp32, and y is in 8 bits with a scale for each row.
  * fftconv_rms_norm_backward: with z = h rstd and g = dy . weight
  *     dx = dh + rstd (g - z mean(g z)),  dweight = sum over rows of dy . z.
  *   dx is the gradient of x and of the residual alike; dh (contiguous, may be NULL) is what comes back along the residual stream; lddy:

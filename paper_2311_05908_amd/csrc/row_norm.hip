@@ -20,6 +20,7 @@ struct RowArgs {
     float *rstd, *scale;
     int64_t T, D, ldx, ldr;
     float eps;
+    double eps64;                 // the same, for rows in other units
     int norm, i8;
 };
 
@@ -80,12 +81,48 @@ template <typename T, int E, int CH, int WPR, bool WHOLE> __global__ void __laun
 #pragma unroll
                 for (int e = 0; e < E; ++e) ss = fmaf(v[c][e], v[c][e], ss);
             ss = __builtin_bit_cast(float, row_reduce<WPR>(__builtin_bit_cast(uint32_t, ss), AddF32(), part, at));
-            const float rstd = 1.f / sqrtf(fmaf(ss, by_d, a.eps));
+            float rstd = 1.f / sqrtf(fmaf(ss, by_d, a.eps));
+            // Squares beyond fp32's largest number, or so small that their own rounding, or that of values below 2^-126, counts (2^-100 and less): the row
+            // once more in units of a power of two near its largest magnitude, what it is divided by in 64 bits.
+            bool own_units = false;
+            if (!(ss < __builtin_inff()) || ss < 0x1p-100f) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) top = MaxU32()(top, magnitude(v[c][e]));
+                top = row_reduce<WPR>(top, MaxU32(), part, at);
+                if (top != 0 && top < 0x7f800000u) {              // (a row of zeros, or with an infinity or NaN, has no such units)
+                    own_units = true;
+                    const int unit = ilogbf(__builtin_bit_cast(float, top));
+                    ss = 0.f;
+#pragma unroll
+                    for (int c = 0; c < CH; ++c)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            v[c][e] = ldexpf(v[c][e], -unit);
+                            ss = fmaf(v[c][e], v[c][e], ss);
+                        }
+                    ss = __builtin_bit_cast(float, row_reduce<WPR>(__builtin_bit_cast(uint32_t, ss), AddF32(), part, at));
+                    const double by = 1.0 / sqrt((double)ss / (double)a.D + ldexp(a.eps64, -2 * unit));
+                    rstd = (float)ldexp(by, -unit);
+#pragma unroll
+                    for (int c = 0; c < CH; ++c)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            float by_w = w[c][e];
+                            asm volatile("" : "+v"(by_w), "+v"(v[c][e]));      // (else all weights are kept in 64 bits throughout)
+                            v[c][e] = (float)((double)v[c][e] * by * (double)by_w);
+                        }
+                }
+            }
             if (a.rstd && lane == 0) a.rstd[row] = rstd;
+            if (!own_units) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+                for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[c][e] = v[c][e] * rstd * w[c][e];
+                    for (int e = 0; e < E; ++e) v[c][e] = v[c][e] * rstd * w[c][e];
+            }
         }
         if (!a.i8) {
 #pragma unroll
@@ -266,7 +303,7 @@ size_t rms_norm_backward_workspace(int64_t T, int64_t D, int dtype)
 int rows_forward(const void *x, int64_t ldx, const void *r, int64_t ldr, const float *w, void *y, void *h, float *rstd, float *scale, int64_t T,
                  int64_t D, double eps, int norm, int i8, int dtype, hipStream_t s)
 {
-    const RowArgs a = {x, r, w, y, h, rstd, scale, T, D, ldx, ldr, (float)eps, norm, i8};
+    const RowArgs a = {x, r, w, y, h, rstd, scale, T, D, ldx, ldr, (float)eps, eps, norm, i8};
     return with_row_kernel(D, dtype, [&](auto t, auto e, auto ch, auto wpr, auto whole) -> int {
         using TY = decltype(t);
         int64_t g = row_groups(T, row_shape(D, dtype));

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2311_05908_amd import fftconv, layers
-from test_layers_gpu import DT, E, RUN, U, gen, int_rows, normal, runs8, weight_check, within
+from test_layers_gpu import DT, E, RUN, U, gen, int_rows, norm_ref, normal, runs8, weight_check, within
 
 pytestmark = pytest.mark.gpu
 
@@ -148,3 +148,52 @@ def test_norm_of_a_slice_goes_back_without_a_residual(dtype):
         assert torch.equal(h, x) and torch.equal(rstd, rc)
         assert all(torch.equal(a, b) for a, b in zip(y, yc))
         assert all(torch.equal(a, b) for a, b in zip(layers.rms_norm_backward(dy, h, w, rstd), layers.rms_norm_backward(dy, hc, w, rc)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [1, 70, 255, 768, 1001, 2048, 4096, 5000, 8193, 16384])
+def test_norm_of_rows_whose_squares_leave_fp32(d, dtype):
+    """Finite rows beyond 1.8e19 and below 1e-19, next to ordinary ones, with eps from 0 up, against the formula in 64 bits: y, h, rstd, 8 bits, the
+    gradients."""
+    g = gen(d)
+    size = torch.tensor([1.0, 1e19, 1e20, 1e30, 2.0 ** 124, 1e-19, 1e-20, 1e-25, 1e-30, 1e-37], device="cuda")
+    x = (normal(g, 10, d).clamp(-7, 7) * size[:, None]).to(DT[dtype])
+    x[x == 0] = 1e-37
+    dy, w = normal(g, 10, d, dtype=DT[dtype]), 1 + 0.1 * normal(g, d)
+    u, c = U[dtype], (d / 64 + 64) * E
+    for eps in (0.0, 1e-70, 1e-50, 1e-40, 1e-30, 1e-6, 1e30):
+        hr, rr, yr = norm_ref(x, None, w, eps)
+        y, h, rstd = layers.rms_norm(x, w, residual=torch.zeros_like(x), eps=eps)
+        assert torch.equal(h, x)
+        within(rstd, rr, c * rr + 2.0 ** -149, "rstd")
+        within(y, yr, (u + c) * yr.abs() + 2.0 ** (-149 if dtype == "f32" else -134), "y")
+        rows, _, _ = layers.rms_norm_i8(x, w, eps=eps)
+        top = yr.abs().amax(-1)
+        tiny = top < 2.0 ** -99
+        within(rows.scale[~tiny], top[~tiny] / 127, c * top[~tiny] / 127, "scale")
+        within(rows.float()[~tiny], yr[~tiny], (top / 127 * (0.5 + 127 * 2 * c))[~tiny, None].expand_as(yr[~tiny]), "8 bits")
+        # (of the rstd that the pass left, which has less than 24 bits where it is subnormal)
+        z, gg, r64 = h.double() * rstd.double()[:, None], dy.double() * w.double(), rstd.double()[:, None]
+        dx, dw = layers.rms_norm_backward(dy, h, w, rstd)
+        ref = r64 * (gg - z * (gg * z).mean(-1, keepdim=True))
+        over = ref.abs().amax(-1) > 1e38                      # (beyond the type)
+        span = r64 * (gg.abs() + z.abs() * (gg * z).abs().mean(-1, keepdim=True))
+        within(dx[~over], ref[~over], (u * ref.abs() + c * span + 2.0 ** (-149 if dtype == "f32" else -134))[~over], "dx")
+        within(dw, (dy.double() * z).sum(0), 80 * E * (dy.double() * z).abs().sum(0), "dw")
+
+
+def test_norm_of_the_smallest_and_largest_numbers():
+    """Subnormal rows with eps = 0, whose rstd no fp32 number holds, and rows of fp32's largest number."""
+    w = torch.ones(300, device="cuda")
+    x = torch.full((4, 300), 2.0 ** -149, device="cuda")
+    x[1] *= torch.arange(1, 301, device="cuda")
+    x[2:] = 3.4028234e38
+    x[3, ::2] *= -1
+    _, _, yr = norm_ref(x, None, w, 0.0)
+    y, h, rstd = layers.rms_norm(x, w, eps=0.0)
+    within(y, yr, 80 * E * yr.abs())
+    assert torch.isinf(rstd[:2]).all()
+    # an infinity or NaN in a row is no finite row: as before
+    x[0, 3], x[2, 5] = float("inf"), float("nan")
+    rows, _, _ = layers.rms_norm_i8(x, w, eps=0.0)
+    assert torch.isnan(rows.scale[[0, 2]]).all() and torch.isfinite(rows.scale[[1, 3]]).all()
