@@ -288,7 +288,8 @@ int fftconv_linear_i8(const int8_t *x, const float *x_scale, const int8_t *w, co
  *     dw[o, c] = sum over b, n of dy[b, n, o] q[b, c, n] scale[b, c, n / 128].
  *   dy: (B, N, O) with tokens = 1, else (B, O, N).  dw: (O, C), fp32 or dtype (dtype_dw).  N, O and C up to 2^22, O C up to 2^36.
  *   A run whose scale is zero stands for zeros, whatever its q.
- *   Products are exact (8-bit values times dy), sums in fp32.  workspace: fftconv_workspace_bytes_linear_grad_weight bytes. */
+ *   Products are exact (8-bit values times dy), sums in fp32, in units of the scales: of dy q, and where a channel's scales differ of up to
+ *   2^60 times it, which has to stay in fp32's range.  An infinity or NaN in dy reaches its own o alone.  workspace: fftconv_workspace_bytes_linear_grad_weight bytes. */
 int fftconv_act_pack(const void *x, int8_t *q, float *scale, int64_t B, int64_t C, int64_t N, int tokens, int dtype, void *stream);
 int fftconv_act_unpack(const int8_t *q, const float *scale, const int8_t *gate_q, const float *gate_scale, const void *gate, void *x, int64_t B,
                        int64_t C, int64_t N, int dtype, void *stream);

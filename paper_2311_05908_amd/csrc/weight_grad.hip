@@ -48,7 +48,8 @@ __device__ __forceinline__ f32x16 mfma16(uint4 a, uint4 b, f32x16 c, _Float16)
 // operand's read takes at once nor the transposed pieces that sixteen lanes write at once meet in a bank.
 __device__ __forceinline__ int place(int row, int c) { return row * 128 + ((c ^ ((row ^ ((row >> 3) & 3)) & 7)) << 4); }
 
-// One 16-bit part after the other of values in T.
+// One 16-bit part after the other of values in T. Of fp32 the upper 8 bits of the fraction each time, cut off rather than rounded: three times 8 are all
+// 24, and no finite number becomes an infinity. An infinity is the first part alone.
 template <typename T, typename P> __device__ __forceinline__ void split(const T &v, P (&o)[Operand<T>::PARTS])
 {
     if constexpr (sizeof(T) == 2) {
@@ -57,8 +58,10 @@ template <typename T, typename P> __device__ __forceinline__ void split(const T 
         float left = v;
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
-            o[p] = (P)left;
-            left -= (float)o[p];
+            const uint32_t upper = __builtin_bit_cast(uint32_t, left) & 0xffff0000u;
+            o[p] = __builtin_bit_cast(P, (uint16_t)(upper >> 16));
+            left -= __builtin_bit_cast(float, upper);
+            if (p == 0) left = magnitude(v) == 0x7f800000u ? 0.f : left;
         }
     }
 }

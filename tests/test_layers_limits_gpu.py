@@ -197,3 +197,43 @@ def test_norm_of_the_smallest_and_largest_numbers():
     x[0, 3], x[2, 5] = float("inf"), float("nan")
     rows, _, _ = layers.rms_norm_i8(x, w, eps=0.0)
     assert torch.isnan(rows.scale[[0, 2]]).all() and torch.isfinite(rows.scale[[1, 3]]).all()
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("layout", ["tokens", "channels"])
+@pytest.mark.parametrize("n,o,c", [(1200, 72, 140), (1201, 72, 140), (2, 1, 1), (640, 1032, 1030)])
+def test_weight_gradient_of_infinities(n, o, c, layout, dtype):
+    """An infinity in dy reaches its own output channel: an infinity of the product's sign, NaN where the 8-bit value is 0 or two of them cancel; NaN is
+    NaN there; everything else is as without them."""
+    g = gen(41)
+    dy = normal(g, 1, n, o, dtype=DT[dtype])
+    q, s = runs8(normal(g, 1, c, n))
+    q[0, c // 2, 0] = 0
+    at = {(0, 0): float("inf")}
+    if o > 1:
+        at.update({(n // 2, 1): float("-inf"), (n - 1, o - 1): float("nan"), (1, 9): float("inf"), (n - 2, 9): float("inf")})
+    plain = dy.clone()
+    for (i, j), v in at.items():
+        dy[0, i, j], plain[0, i, j] = v, 0
+    turned = (lambda t: t) if layout == "tokens" else (lambda t: t.transpose(1, 2).contiguous())
+    got = layers.linear_grad_weight(turned(dy), (q, s), layout=layout)
+    x = q[0].double() * s[0].double().repeat_interleave(RUN, -1)[..., :n]
+    want = layers.linear_grad_weight(turned(plain), (q, s), layout=layout).double()
+    for (i, j), v in at.items():
+        want[j] += v * x[:, i]
+    assert torch.equal(torch.nan_to_num(got.double(), nan=12345.0), torch.nan_to_num(want, nan=12345.0))
+
+
+@pytest.mark.parametrize("layout", ["tokens", "channels"])
+def test_weight_gradient_of_the_largest_numbers(layout):
+    """fp32 dy above bf16's largest number, and every other 24-bit number: no part of it is lost or an infinity."""
+    g = gen(42)
+    n, o, c = 130, 40, 9
+    dy = torch.zeros(1, n, o, device="cuda")
+    big = torch.tensor([3.4028234e38, 3.39e38, 3.3961775e38, 2.0 ** 127, -3.4028234e38, 1.1754944e-38, 1.5e-30, -1e30], device="cuda")
+    dy[0, torch.arange(o, device="cuda") * 3, torch.arange(o, device="cuda")] = big.repeat(5)
+    q = torch.where(torch.rand(1, c, n, generator=g, device="cuda") < 0.5, -1, 1).to(torch.int8)
+    s = torch.full((1, c, 2), 0.5, device="cuda")
+    got = layers.linear_grad_weight(dy if layout == "tokens" else dy.transpose(1, 2).contiguous(), (q, s), layout=layout)
+    ref = dy[0].double().T @ (q[0].double().T * 0.5)
+    within(got, ref, 3 * E * ref.abs() + 2.0 ** -133)
