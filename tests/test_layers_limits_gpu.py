@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2311_05908_amd import fftconv, layers
-from test_layers_gpu import DT, E, RUN, U, gen, int_rows, norm_ref, normal, runs8, weight_check, within
+from test_layers_gpu import DT, E, RUN, U, gen, int_rows, norm_ref, normal, runs8, unpacked, weight_check, within
 
 pytestmark = pytest.mark.gpu
 
@@ -237,3 +237,41 @@ def test_weight_gradient_of_the_largest_numbers(layout):
     got = layers.linear_grad_weight(dy if layout == "tokens" else dy.transpose(1, 2).contiguous(), (q, s), layout=layout)
     ref = dy[0].double().T @ (q[0].double().T * 0.5)
     within(got, ref, 3 * E * ref.abs() + 2.0 ** -133)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("layout", ["tokens", "channels"])
+@pytest.mark.parametrize("b,n,o,c", [(4, 4096, 130, 200), (3, 5000, 520, 300), (4, 4096, 1152, 1030), (5, 3001, 1101, 1040), (200, 17, 64, 70)])
+def test_weight_gradient_of_whole_numbers_is_exact(b, n, o, c, layout, dtype):
+    """Whole numbers whose sums of magnitudes stay below 2^24, scales that are powers of two: every sum on the way is a number that fp32 holds, so the result
+    is the formula's in every bit, however many terms there are and in whatever order. (Worst-case bounds grow with the terms and would let much pass.)"""
+    g = gen(51)
+    top = (1 << 24) // (b * n * 127)
+    assert top >= 3
+    dy = torch.randint(-min(top, 127), min(top, 127) + 1, (b, n, o), generator=g, device="cuda").to(DT[dtype])
+    q = torch.randint(-127, 128, (b, c, n), generator=g, device="cuda", dtype=torch.int32).to(torch.int8)
+    s = torch.ones(b, c, -(-n // RUN), device="cuda") * 2.0 ** -torch.arange(c, device="cuda").remainder(20).float()[:, None]
+    ref = dy.reshape(-1, o).double().T @ unpacked(q, s).permute(0, 2, 1).reshape(-1, c)
+    got = layers.linear_grad_weight(dy if layout == "tokens" else dy.transpose(1, 2).contiguous(), (q, s), layout=layout)
+    assert torch.equal(got.double(), ref)
+    got = layers.linear_grad_weight(dy if layout == "tokens" else dy.transpose(1, 2).contiguous(), (q, s), layout=layout, dtype=DT[dtype])
+    assert torch.equal(got, ref.to(DT[dtype]))
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("layout", ["tokens", "channels"])
+@pytest.mark.parametrize("b,n,o,c", [(2, 4096, 130, 200), (2, 1201, 72, 140), (2, 4096, 1152, 1030)])
+def test_weight_gradient_keeps_all_bits_of_dy(b, n, o, c, layout, dtype):
+    """One sample of dy to an output channel, numbers of all of the type's bits and of sizes down to its subnormal ones: a result is one product, rounded where
+    its parts are added up, not more. A part of fp32's 24 bits left out would be 2^-16 of it."""
+    g = gen(52)
+    value = normal(g, o).to(DT[dtype])
+    value[::5] *= 2.0 ** {"f16": -14, "bf16": -60, "f32": -60}[dtype]
+    dy = torch.zeros(b, n, o, dtype=DT[dtype], device="cuda")
+    at = torch.randint(0, b * n, (o,), generator=g, device="cuda")
+    dy.reshape(-1, o)[at, torch.arange(o, device="cuda")] = value
+    q = torch.randint(1, 128, (b, c, n), generator=g, device="cuda", dtype=torch.int32).to(torch.int8)
+    s = torch.full((b, c, -(-n // RUN)), 2.0 ** -3, device="cuda")
+    ref = value.double()[:, None] * unpacked(q, s).permute(0, 2, 1).reshape(-1, c)[at]
+    got = layers.linear_grad_weight(dy if layout == "tokens" else dy.transpose(1, 2).contiguous(), (q, s), layout=layout)
+    within(got, ref, 3 * E * ref.abs())
