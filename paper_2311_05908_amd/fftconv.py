@@ -172,14 +172,16 @@ def _extension():
 
 @functools.lru_cache(maxsize=None)
 def _fastcall():
-    """call() of the binding's extension, which is built first if there is none; None where it cannot be."""
+    """call() of the binding's extension, which is built first if there is none; None where it cannot be, or where what is there was built before it took
+    as many arguments as the operators around the convolutions have (call_norm came with them)."""
     if not os.path.exists(_build.fastcall_path()):
         _build.try_build_fastcall()
         importlib.invalidate_caches()
     try:
-        return _extension().call
+        extension = _extension()
     except ImportError:
         return None
+    return extension.call if hasattr(extension, "call_norm") else None
 
 
 @functools.lru_cache(maxsize=None)      # (of six entry points a plan: 5 of the 90 us that a plan of short rows takes)

@@ -99,11 +99,10 @@ def _calls(lib):
     fast = _f._fastcall()
     c = {name: _f._entry(lib, "fftconv_" + name) for name in ("rms_norm_backward", "linear_i8", "act_pack", "act_unpack", "linear_grad_weight")}
     c["quantize_rows"] = lib.fftconv_quantize_rows
-    norm = getattr(_f._extension(), "call_norm", None) if fast else None
-    if norm is None:
+    if fast is None:
         c["rms_norm"] = lambda eps, *a: lib.fftconv_rms_norm(*a[:11], eps, *a[11:])
     else:
-        c["rms_norm"] = functools.partial(norm, ctypes.cast(lib.fftconv_rms_norm, ctypes.c_void_p).value)
+        c["rms_norm"] = functools.partial(_f._extension().call_norm, ctypes.cast(lib.fftconv_rms_norm, ctypes.c_void_p).value)
     return type("Calls", (), {k: staticmethod(v) for k, v in c.items()})
 
 
