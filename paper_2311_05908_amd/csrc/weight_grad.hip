@@ -336,7 +336,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
             // units so much smaller that the sums might leave fp32's range: the sums so far are put aside
             bool small = false;
 #pragma unroll
-            for (int j = 0; j < FC; ++j) small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
+            for (int j = 0; j < FC; ++j) small |= s[j] != 0.f && fabsf(s[j]) < top[j] * 0x1p-60f;
             if (__builtin_amdgcn_ballot_w64(small) != 0) break;
             zeros = 0;
 #pragma unroll
@@ -345,7 +345,7 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
                 zeros |= (s[j] == 0.f ? 1u : 0u) << j;
                 const float f = s[j] == 0.f || unit[j] == 0.f ? 1.f : unit[j] / s[j];
                 unit[j] = s[j] == 0.f ? unit[j] : s[j];
-                top[j] = fmaxf(top[j], unit[j]);
+                top[j] = fmaxf(top[j], fabsf(unit[j]));
 #pragma unroll
                 for (int i = 0; i < FO; ++i) acc[i][j] *= f;
             }
@@ -566,13 +566,13 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
         for (; blk < last; ++blk) {
             bool small = false;
 #pragma unroll
-            for (int j = 0; j < FC; ++j) small |= s[j] > 0.f && s[j] < top[j] * 0x1p-60f;
+            for (int j = 0; j < FC; ++j) small |= s[j] != 0.f && fabsf(s[j]) < top[j] * 0x1p-60f;
             if (__builtin_amdgcn_ballot_w64(small) != 0) break;
 #pragma unroll
             for (int j = 0; j < FC; ++j) {
                 const float f = s[j] == 0.f || unit[j] == 0.f ? 1.f : unit[j] / s[j];
                 unit[j] = s[j] == 0.f ? unit[j] : s[j];
-                top[j] = fmaxf(top[j], unit[j]);
+                top[j] = fmaxf(top[j], fabsf(unit[j]));
 #pragma unroll
                 for (int i = 0; i < FO; ++i) acc[i][j] *= f;
             }

@@ -275,3 +275,19 @@ def test_weight_gradient_keeps_all_bits_of_dy(b, n, o, c, layout, dtype):
     ref = value.double()[:, None] * unpacked(q, s).permute(0, 2, 1).reshape(-1, c)[at]
     got = layers.linear_grad_weight(dy if layout == "tokens" else dy.transpose(1, 2).contiguous(), (q, s), layout=layout)
     within(got, ref, 3 * E * ref.abs())
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("layout", ["tokens", "channels"])
+@pytest.mark.parametrize("n", [1200, 1201])
+def test_weight_gradient_of_negative_scales(n, layout, dtype):
+    """Scales that no call leaves but that the formula holds for: of either sign, 2^120 apart, so that sums in units of the smaller ones leave fp32."""
+    g = gen(91)
+    b, o, c = 3, 1032, 1030
+    dy = normal(g, b, n, o, dtype=DT[dtype])
+    q, s = runs8(normal(g, b, c, n))
+    s[:, 1::4, 1::2] *= -(2.0 ** -120)
+    s[:, 2::4, ::2] *= -1
+    s[:, 3::4] *= -1
+    s[:, 3::4, 1::2] *= 2.0 ** -120
+    weight_check(dy if layout == "tokens" else dy.transpose(1, 2).contiguous(), q, s, layout, "f32")
