@@ -244,8 +244,9 @@ int fftconv_backward_filter(const fftconv_plan *plan, const void *u, const void 
  * gradient of a projection's weight) and for serving (norm with 8-bit rows, 8-bit projections, down to single tokens).  They take no
  * plan; the conventions are those at the top: device pointers, asynchronous on `stream`, nothing allocated, no synchronisation, a code
  * returned, nothing launched on error.  Tensors need only the alignment of their element type (16 bytes is faster), and no output
- * overlaps an input.  Sums, statistics and scales are fp32 or 32-bit integers; every value is rounded once, to nearest even, where it is
- * written.  Results do not depend on timing: every sum has an order that the sizes alone decide.
+ * overlaps an input.  Sums of 8-bit products are 32-bit integers; everything else is fp32, an operation after the other, each rounded (the
+ * steps of a formula have to stay in fp32's range), and a result is rounded to its type, to nearest even, where it is written.  Results do
+ * not depend on timing: every sum has an order that sizes, types and the tensors' alignment decide.
  *
  * 8-bit values: q = x / s rounded to the nearest integer, ties to even, with s = max |x| / 127 over the values that share the scale, so
  * q is in [-127, 127] (-128 is accepted where 8-bit values are read).  Where max |x| is below 2^-100, s and q are 0.  Where a value is
@@ -256,7 +257,8 @@ int fftconv_backward_filter(const fftconv_plan *plan, const void *u, const void 
  *   residual may be NULL (h = x).  ldx, ldr: distance between rows of x and of the residual in elements, >= D.  weight: D fp32.  y, h:
  *   contiguous; h (the residual stream for the next layer, rounded to dtype; the norm is taken of the sum before that) and rstd (T
  *   fp32, for the backward pass) may be NULL.  Rows may hold any finite numbers: where their squares leave fp32 the row is taken in
- *   units of its own (rstd is then what fp32 holds of it, infinity for rows below 3e-39 with eps = 0).  scale: NULL, and y is in dtype; or T fp32, and y is in 8 bits with a scale for each row.
+ *   units of its own (rstd is then what fp32 holds of it, infinity for rows below 3e-39 with eps = 0).
+ *   scale: NULL, and y is in dtype; or T fp32, and y is in 8 bits with a scale for each row.
  * fftconv_rms_norm_backward: with z = h rstd and g = dy . weight
  *     dx = dh + rstd (g - z mean(g z)),  dweight = sum over rows of dy . z.
  *   dx is the gradient of x and of the residual alike; dh (contiguous, may be NULL) is what comes back along the residual stream; lddy:
@@ -271,7 +273,9 @@ int fftconv_quantize_rows(const void *x, int64_t ldx, int8_t *q, float *scale, i
 
 /* Projection in 8 bits: for the tokens t = (b, n) of B sequences of N samples
  *     y[t, o] = (sum over k of x[t, k] w[o, k]) x_scale[t] w_scale[o] + bias[o],
- * the sum in 32-bit integers, exact.  x: (B, N, K), w: (O, K), contiguous; bias: O fp32 or NULL; 1 <= K <= 131071; B N and O up to 2^31 - 512, B N O up to 2^42.
+ * the sum in 32-bit integers, exact.  x: (B, N, K), w: (O, K), contiguous; bias: O fp32 or NULL; 1 <= K <= 131071; B N
+ * and O up to 2^31 - 512, B N O up to 2^42.  The sum is rounded to fp32 and multiplied by one scale; the product with the other and the bias'
+ * addition are rounded together (which scale comes first depends on the layout of y).
  *   parts = 0: y is (B, N, O), token by token.  parts >= 1, a divisor of O: y is (parts, B, O / parts, N), channel by channel, what the
  *   convolutions take: with parts = 3, u, w and v of fftconv_forward_gated lie one after the other.  dtype: of y.
  *   workspace: fftconv_workspace_bytes_linear_i8 bytes (may be NULL when that is 0). */
@@ -289,7 +293,8 @@ int fftconv_linear_i8(const int8_t *x, const float *x_scale, const int8_t *w, co
  *   dy: (B, N, O) with tokens = 1, else (B, O, N).  dw: (O, C), fp32 or dtype (dtype_dw).  N, O and C up to 2^22, O C up to 2^36.
  *   A run whose scale is zero stands for zeros, whatever its q.
  *   Products are exact (8-bit values times dy), sums in fp32, in units of the scales: of dy q, and where a channel's scales differ of up to
- *   2^60 times it, which has to stay in fp32's range.  An infinity or NaN in dy reaches its own o alone.  workspace: fftconv_workspace_bytes_linear_grad_weight bytes. */
+ *   2^60 times it, which has to stay in fp32's range.  An infinity or NaN in dy reaches its own o alone.
+ *   workspace: fftconv_workspace_bytes_linear_grad_weight bytes. */
 int fftconv_act_pack(const void *x, int8_t *q, float *scale, int64_t B, int64_t C, int64_t N, int tokens, int dtype, void *stream);
 int fftconv_act_unpack(const int8_t *q, const float *scale, const int8_t *gate_q, const float *gate_scale, const void *gate, void *x, int64_t B,
                        int64_t C, int64_t N, int dtype, void *stream);

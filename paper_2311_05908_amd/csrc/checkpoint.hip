@@ -1,7 +1,7 @@
 // Activations kept for the backward pass in 8 bits: (B, C, N) with a scale for every 128 samples of a channel, and back.
 //
 //   s[b, c, j] = max |x[b, c, n]| / 127 over the run n = 128 j ... 128 j + 127,  q = round(x / s)
-//   x^ = q s, or the product of two such with one rounding at the end (u . w, as the gradient of a gated convolution's filter takes it)
+//   x^ = q s, or the product of two such, in fp32, rounded to its type at the end (u . w, as the gradient of a gated convolution's filter takes it)
 //
 // Runs lie along the samples because that is the direction every gradient here sums over (a filter's, a projection's): within a run
 // the scale comes out of the sum. Bound by the bytes moved: bf16 64 x 768 x 4096 packed in 129 us (4.7 TB/s), read back as a product in 129 us (6.2).
@@ -53,8 +53,8 @@ template <typename T, bool WHOLE> __global__ void __launch_bounds__(256) k_pack(
 
 // The same from (B, N, C): a workgroup takes one run of 64 channels and turns it over in LDS. Thread t reads 8 channels (t % 8) of the four samples
 // 4 (t / 8) ...; the largest magnitude of a channel is taken over its four samples, over the eight threads of the wave with the same channels by
-// exchanges, and over the four waves by way of LDS. bf16 64 x 4096 x 768: 189 us, 3.2 TB/s (199 with LDS's atomic maximum): more than the bytes,
-// for the steps of a workgroup follow each other.
+// exchanges, and over the four waves by way of LDS. bf16 64 x 4096 x 768, three tensors in turn: 167 us, 3.6 TB/s, where
+// k_pack takes 131: the steps of a workgroup follow each other.
 template <typename T> __global__ void __launch_bounds__(256) k_pack_tokens(const T *__restrict__ x, int8_t *__restrict__ q, float *__restrict__ scale,
                                                                             int64_t C, int64_t N, uint32_t runs, uint32_t cgroups, uint32_t first)
 {

@@ -152,7 +152,7 @@ __device__ __forceinline__ int8_t quantised(float x, float s) { return s > 0.f ?
 
 // The same for E values (4 or 8) of one scale. |x / s| is at most 127 and a bit, so x (1 / s), not rounded before 1.5 2^23 is added, is within
 // 127 2^-24 of the quotient: its nearest integer, which that sum holds in its lowest bits, is the quotient's unless it lies within 2^-14 of a tie.
-// Only there the quotient itself is taken (a wave in thirty or so): five instructions a value instead of fifteen.
+// Only there the quotient itself is taken (a wave in sixteen or so for eight values a lane): five instructions a value instead of fifteen.
 template <int E> __device__ __forceinline__ void quantise(const float (&x)[E], float s, int8_t (&q)[E])
 {
     constexpr float SHIFT = 12582912.f;

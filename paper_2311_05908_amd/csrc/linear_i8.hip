@@ -1,14 +1,16 @@
 // Product of rows in 8 bits with a weight in 8 bits, a scale for each token and for each output channel:
 //
-//   y[t, o] = (sum over k of x[t, k] w[o, k]) xs[t] ws[o] + bias[o]        the sum in 32-bit integers, exact; one rounding, at the store
+//   y[t, o] = (sum over k of x[t, k] w[o, k]) xs[t] ws[o] + bias[o]        the sum in 32-bit integers, exact, the rest in fp32, rounded at the store
 //
 // One kernel serves both layouts of y. Its two operands, both with k contiguous, are R, whose rows lie next to each other in y, and S:
 // token by token (t, o) R is the weight, channel by channel (parts, b, o / parts, n) R is the tokens. An accumulator of the matrix cores holds
 // four consecutive rows of R for one row of S in a lane, so the values that a lane stores are neighbours in y either way.
 //
-// Which kernel: up to 64 tokens k_linear_few, bound by the weight's bytes; above, with k in pieces of 16 bytes, k_linear_async on tiles of 256 x 256
-// where there is one for every compute unit, else of 128 x 128, with k in ranges where there are few of those; else k_linear, which takes any k
-// at any alignment (4097 x 4097 -> 4097: 0.69 POP/s, where 4096 x 4096 -> 4096 makes 1.96).
+// Which kernel: up to 64 tokens k_linear_few, bound by the weight's bytes. Above, with k in pieces of 16 bytes (both operands aligned to them),
+// k_linear_async: on tiles of 256 x 256 where there is one for every compute unit, else on 128 x 128 where there are 128 of those, and with k in ranges
+// where there are 64 or less and k is about 1000 or more. Everything else is k_linear's, which takes any k at any alignment, on up to 128 x 256 (4097 x
+// 4097 -> 4097: 0.72 POP/s, where 4096 x 4096 -> 4096 makes 2.1): among it calls of 65 to 127 tiles of 128 x 128, or of fewer with a shorter k, on 64 x 64.
+// That last line has not been measured out: 4096 -> 4096 takes 20 us for 256 tokens (ranges), 39 for 257 to 384 (k_linear) and 19 for 385.
 #include "async_lds.h"
 #include "layers_index.h"
 
@@ -259,11 +261,12 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) 
 // operands in registers one group ahead. A workgroup takes one tile after the other without a pause in the stream of pieces: what is asked for
 // during a tile's last steps is the next tile's, so its first loads are not waited for.
 //
-// Measured: f16 8192 x 4096 -> 16384 501 us, 2.2 POP/s; bf16 64 x 4096 x 768 -> 3 x 768 620 us, 1.5 POP/s, with 1.2 GB written. The matrix cores alone,
-// with nothing brought or stored, take 425 and 330 us of that: at their full rate the board's power lets the clock fall to 1.3 GHz, so what is
-// brought (70 and 60 us), scaled (100) and stored (150) comes on top rather than beside them, and fewer bytes and instructions count, not
-// waits: without any wait for a transfer, or without barriers, the time is the same. Hence the large tile (128 x 128: 741 and 917 us), whole
-// lines to a store, and places in y that cost no arithmetic.
+// Measured: f16 8192 x 4096 -> 16384 505 us, 2.2 POP/s; bf16 64 x 4096 x 768 -> 3 x 768 613 us, 1.5 POP/s, with 1.2 GB written. Back to back the socket
+// is at its cap (1391 and 1398 of 1400 W); under the profiler, which pauses between launches, 492 and 560 us at 1.9 GHz, the matrix cores busy 55 and
+// 41 % of it. The matrix cores alone, with nothing brought or stored, take 425 and 330 us; what is brought (70 and 60 us), scaled (100)
+// and stored (150) comes on top rather than beside them, for results are written after a tile's products; without any wait for a transfer, or
+// without barriers, the time is the same. Hence the large tile (128 x 128: 741 and 917 us), whole lines to a store, and places in y that cost
+// no arithmetic.
 //
 // Which tile: workgroups go to the dies in turn; a die takes a stretch of the tiles, its workgroups side by side, in an order in which
 // neighbours share rows of R or of S, so that those come from its L2.

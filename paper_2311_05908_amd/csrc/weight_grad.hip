@@ -11,7 +11,7 @@
 //
 // Which kernel: k_weight_async for 16-bit dy in pieces of 16 bytes, k_weight for everything else (fp32, odd lengths, any alignment): it stages
 // dy and q through registers, where it turns dy over, widens q and splits fp32, four waves before the products of a half run and four after
-// them. bf16 8 x 4095, 1024 x 4096: 341 us, where 8 x 4096 takes 318 on the other one.
+// them. bf16 8 x 4095, 1024 x 4096: 335 us, where 8 x 4096 takes 318 on the other one.
 #include "async_lds.h"
 #include "layers_index.h"
 
@@ -375,10 +375,10 @@ template <typename T, bool TOKENS, typename DW, int FO, int FC> __global__ void 
 // Samples of a half run, as operands want them (8 for a lane of either half of the wave): pair u of products, product v of it, takes
 // 32 u + 16 half + 8 v ..., so that one read of 16 bytes of q serves both.
 //
-// Measured: bf16 64 x 4096, 2304 x 768: 0.98 ms, 0.95 PFLOP/s. The products alone take 574 us of it (1.6 PFLOP/s, the board's limit of power); what is
-// brought costs 225 us (70 of them because it comes from beyond the L2), widening q 115, the quotients of the scales 72, reading dy from LDS 55:
-// each leaves when it is left out, and waits cost nothing. Taking turns (one wave of a SIMD reads and widens while the other multiplies, a
-// barrier at each turn) was slower, 1.14 ms.
+// Measured: bf16 64 x 4096, 2304 x 768: 0.99 ms and 11 us for the sums, 0.92 PFLOP/s; back to back the socket is at 1382 of 1400 W. Under the profiler,
+// which pauses between launches, 0.91 ms at 2.25 GHz, the matrix cores busy 43 % of it and other vector instructions' issue 42. The products alone take
+// 574 us (1.6 PFLOP/s); what is brought costs 225 us (70 of them because it comes from beyond the L2), widening q 115, the quotients of the scales 72,
+// reading dy from LDS 55: each leaves when it is left out, and waits cost nothing. Taking turns (one wave of a SIMD reads and widens while the other multiplies, a barrier at each turn) was slower, 1.14 ms.
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 __device__ __forceinline__ uint2 read_transposed(const char *p)
 {

@@ -252,7 +252,7 @@ def _kept(name, p):
 
 def act_unpack(p, dtype=torch.bfloat16, gate=None):
     """fftconv_act_unpack: the activations of a Checkpoint8 (or a pair (q, scale)), (b, c, n) in dtype; times `gate`, a second one or a tensor in
-    dtype, with one rounding."""
+    dtype, the product in fp32."""
     q, scale = _kept("the checkpoint", p)
     if dtype not in _f._DTYPE_CODE:
         raise ValueError("dtype must be fp32, fp16 or bf16")
