@@ -302,6 +302,33 @@ size_t fftconv_workspace_bytes_linear_grad_weight(int64_t B, int64_t N, int64_t 
 int fftconv_linear_grad_weight(const void *dy, const int8_t *q, const float *scale, void *dw, int64_t B, int64_t N, int64_t O, int64_t C,
                                int tokens, int dtype, int dtype_dw, void *workspace, void *stream);
 
+/* Gated linear recurrence: what mixes the samples of a channel in the convolution's place, with a state that goes on from one call to the
+ * next.  With gates a and inputs x made of u and w,
+ *     gate = FFTCONV_GATE_SIGMOID:  a = sigmoid(w),        x = (1 - a) u
+ *     gate = FFTCONV_GATE_LOG:      a = exp(min(w, 0)),    x = u            (w = -infinity begins anew at its sample)
+ *     h[t] = a[t] h[t-1] + x[t],  h[-1] = state;   y = v . h
+ *   u, w, v, y: (B, C, N) contiguous, in dtype, the layout of u, w and v of fftconv_forward_gated; v may be NULL (y = h).  state, last: (B, C)
+ *   fp32, the state before the first sample (NULL: zeros) and, where not NULL, the one after the last.  lengths: B int32, or NULL (all N):
+ *   sequence b has lengths[b] samples (cut to 0 .. N); what lies behind them is not used, y there is zero and `last` the state after the
+ *   sequence's own last sample.  kept: NULL, or (B, C, ceil(N / 512)) fp32 for the backward pass: the state before every 512th sample.
+ *   The state is fp32 throughout.  From a sample on whose u or w is not a finite number (an infinite w apart), and that h meets, h is an
+ *   infinity or NaN.  Rows in the order of their maps' products: results do not depend on timing.
+ * fftconv_gated_scan_backward: with dy, and dlast the gradient of `last` (NULL: zeros),
+ *     p[t] = a[t] dh[t],  dh[t] = v[t] dy[t] + p[t+1],  p[N] = dlast;  dstate = p[0];  dv = dy . h
+ *     sigmoid: du = (1 - a) dh, dw = dh (h[t-1] - u) a (1 - a);   log: du = dh, dw = dh h[t-1] a (0 where w > 0)
+ *   h is recomputed from u, w and kept.  dv is NULL exactly where v is; dstate may be NULL.  Gradients behind a sequence's end are zero.
+ * fftconv_gated_step: one sample for each of T = B C channels: next = a state + x, y = v next.  next may be state itself.
+ *   B C below 2^31, N below 2^31; workspace: fftconv_workspace_bytes_gated_scan bytes for either pass (may be NULL when that is 0). */
+enum { FFTCONV_GATE_SIGMOID = 0, FFTCONV_GATE_LOG = 1 };
+size_t fftconv_workspace_bytes_gated_scan(int64_t B, int64_t C, int64_t N, int dtype);
+int fftconv_gated_scan(const void *u, const void *w, const void *v, const float *state, const int32_t *lengths, void *y, float *last, float *kept,
+                       int64_t B, int64_t C, int64_t N, int gate, int dtype, void *workspace, void *stream);
+int fftconv_gated_scan_backward(const void *dy, const void *u, const void *w, const void *v, const float *kept, const float *dlast,
+                                const int32_t *lengths, void *du, void *dw, void *dv, float *dstate, int64_t B, int64_t C, int64_t N, int gate,
+                                int dtype, void *workspace, void *stream);
+int fftconv_gated_step(const void *u, const void *w, const void *v, const float *state, float *next, void *y, int64_t T, int gate, int dtype,
+                       void *stream);
+
 /* Fraction of k_f that a cut-off pattern zeroes (Appendix A.4): k_f is viewed
  * as an ndim-dimensional array of shape dims[0..ndim) and, in every dimension
  * i, the last cuts[i] indices are set to zero (cuts[i] = how much of that

@@ -9,7 +9,7 @@ typedef int64_t i;
 
 static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
-    i a[14] = {0};
+    i a[18] = {0};
     int rc = 0;
     (void)self;
     if (n < 1) {
@@ -22,7 +22,7 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
         return NULL;
     }
     --n;
-    if (n != 5 && n != 9 && n != 10 && n != 11 && n != 13 && n != 14) {
+    if (n != 5 && n != 9 && n != 10 && n != 11 && n != 13 && n != 14 && n != 15 && n != 18) {
         PyErr_Format(PyExc_TypeError, "call: no entry point takes %zd arguments", n);
         return NULL;
     }
@@ -40,9 +40,17 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
     case 13:
         rc = ((int (*)(i, i, i, i, i, i, i, i, i, i, i, i, i))f)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12]);
         break;
-    default:
+    case 14:
         rc = ((int (*)(i, i, i, i, i, i, i, i, i, i, i, i, i, i))f)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12],
                                                                   a[13]);
+        break;
+    case 15:
+        rc = ((int (*)(i, i, i, i, i, i, i, i, i, i, i, i, i, i, i))f)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11],
+                                                                     a[12], a[13], a[14]);
+        break;
+    default:
+        rc = ((int (*)(i, i, i, i, i, i, i, i, i, i, i, i, i, i, i, i, i, i))f)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10],
+                                                                              a[11], a[12], a[13], a[14], a[15], a[16], a[17]);
     }
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
@@ -80,4 +88,12 @@ static PyMethodDef methods[] = {{"call_norm", (PyCFunction)(void (*)(void))call_
                                 {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
-PyMODINIT_FUNC PyInit__fastcall(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__fastcall(void)
+{
+    PyObject *const m = PyModule_Create(&module);
+    if (m && PyModule_AddIntConstant(m, "most_arguments", 18) < 0) {
+        Py_DECREF(m);
+        return NULL;
+    }
+    return m;
+}

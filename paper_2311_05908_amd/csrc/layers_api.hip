@@ -81,6 +81,15 @@ int check_weight(const char *who, int64_t B, int64_t N, int64_t O, int64_t C, in
     return FFTCONV_OK;
 }
 
+int check_scan(const char *who, int64_t B, int64_t C, int64_t N, int gate, int dtype)
+{
+    if (!known(dtype)) return bad(who, "unknown dtype");
+    if (gate != FFTCONV_GATE_SIGMOID && gate != FFTCONV_GATE_LOG) return bad(who, "unknown gate");
+    if (B < 0 || C < 1 || N < 1 || N > MOST || times(B, C) < 0) return bad(who, "B >= 0, C >= 1 and N >= 1 are wanted, B C and N below 2^31");
+    if (times(B * C, N, INT64_MAX / 64) < 0) return bad(who, "too many values");
+    return FFTCONV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -187,6 +196,57 @@ int fftconv_linear_grad_weight(const void *dy, const int8_t *q, const float *sca
     if (!aligned(dy, size_of(dtype)) || !aligned(scale, 4) || !aligned(dw, size_of(dtype_dw)) || !aligned(workspace, 4))
         return bad(who, "a tensor is not aligned to its elements");
     return lay::weight_grad(dy, q, scale, dw, B, N, O, C, tokens != 0, dtype, dtype_dw, workspace, (hipStream_t)stream);
+}
+
+size_t fftconv_workspace_bytes_gated_scan(int64_t B, int64_t C, int64_t N, int dtype)
+{
+    if (check_scan("fftconv_workspace_bytes_gated_scan", B, C, N, FFTCONV_GATE_LOG, dtype) != FFTCONV_OK) return 0;
+    return lay::gated_scan_workspace(B * C, N);
+}
+
+int fftconv_gated_scan(const void *u, const void *w, const void *v, const float *state, const int32_t *lengths, void *y, float *last, float *kept,
+                       int64_t B, int64_t C, int64_t N, int gate, int dtype, void *workspace, void *stream)
+{
+    const char *const who = "fftconv_gated_scan";
+    FC_TRY(check_scan(who, B, C, N, gate, dtype));
+    if (B == 0) return FFTCONV_OK;
+    if (!u || !w || !y) return bad(who, "a tensor is NULL");
+    const int64_t to = size_of(dtype);
+    if (!aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(y, to) || !aligned(state, 4) || !aligned(lengths, 4) || !aligned(last, 4) ||
+        !aligned(kept, 4) || !aligned(workspace, 8))
+        return bad(who, "a tensor is not aligned to its elements");
+    if (!workspace && lay::gated_scan_workspace(B * C, N) != 0) return bad(who, "the workspace is NULL");
+    return lay::gated_scan(u, w, v, state, lengths, y, last, kept, B, C, N, gate, dtype, workspace, (hipStream_t)stream);
+}
+
+int fftconv_gated_scan_backward(const void *dy, const void *u, const void *w, const void *v, const float *kept, const float *dlast,
+                                const int32_t *lengths, void *du, void *dw, void *dv, float *dstate, int64_t B, int64_t C, int64_t N, int gate,
+                                int dtype, void *workspace, void *stream)
+{
+    const char *const who = "fftconv_gated_scan_backward";
+    FC_TRY(check_scan(who, B, C, N, gate, dtype));
+    if ((v != nullptr) != (dv != nullptr)) return bad(who, "dv goes with v");
+    if (B == 0) return FFTCONV_OK;
+    if (!dy || !u || !w || !kept || !du || !dw) return bad(who, "a tensor is NULL");
+    const int64_t to = size_of(dtype);
+    if (!aligned(dy, to) || !aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(du, to) || !aligned(dw, to) || !aligned(dv, to) ||
+        !aligned(kept, 4) || !aligned(dlast, 4) || !aligned(lengths, 4) || !aligned(dstate, 4) || !aligned(workspace, 8))
+        return bad(who, "a tensor is not aligned to its elements");
+    if (!workspace && lay::gated_scan_workspace(B * C, N) != 0) return bad(who, "the workspace is NULL");
+    return lay::gated_scan_backward(dy, u, w, v, kept, dlast, lengths, du, dw, dv, dstate, B, C, N, gate, dtype, workspace, (hipStream_t)stream);
+}
+
+int fftconv_gated_step(const void *u, const void *w, const void *v, const float *state, float *next, void *y, int64_t T, int gate, int dtype,
+                       void *stream)
+{
+    const char *const who = "fftconv_gated_step";
+    FC_TRY(check_scan(who, T, 1, 1, gate, dtype));
+    if (T == 0) return FFTCONV_OK;
+    if (!u || !w || !state || !next || !y) return bad(who, "a tensor is NULL");
+    const int64_t to = size_of(dtype);
+    if (!aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(y, to) || !aligned(state, 4) || !aligned(next, 4))
+        return bad(who, "a tensor is not aligned to its elements");
+    return lay::gated_step(u, w, v, state, next, y, T, gate, dtype, (hipStream_t)stream);
 }
 
 }  // extern "C"

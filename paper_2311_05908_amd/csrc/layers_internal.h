@@ -34,5 +34,14 @@ size_t weight_grad_workspace(int64_t B, int64_t N, int64_t O, int64_t C, int dty
 int weight_grad(const void *dy, const int8_t *q, const float *scale, void *dw, int64_t B, int64_t N, int64_t O, int64_t C, bool tokens,
                 int dtype_dy, int dtype_dw, void *workspace, hipStream_t s);
 
+// gated_scan.hip
+size_t gated_scan_workspace(int64_t rows, int64_t N);
+int gated_scan(const void *u, const void *w, const void *v, const float *state, const int32_t *lengths, void *y, float *last, float *kept, int64_t B,
+               int64_t C, int64_t N, int gate, int dtype, void *workspace, hipStream_t s);
+int gated_scan_backward(const void *dy, const void *u, const void *w, const void *v, const float *kept, const float *dlast, const int32_t *lengths,
+                        void *du, void *dw, void *dv, float *dstate, int64_t B, int64_t C, int64_t N, int gate, int dtype, void *workspace,
+                        hipStream_t s);
+int gated_step(const void *u, const void *w, const void *v, const float *state, float *next, void *y, int64_t T, int gate, int dtype, hipStream_t s);
+
 }  // namespace lay
 }  // namespace fftconv

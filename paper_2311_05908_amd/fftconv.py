@@ -31,6 +31,7 @@ EXPORTS = [
     "fftconv_rms_norm", "fftconv_workspace_bytes_rms_norm_backward", "fftconv_rms_norm_backward", "fftconv_quantize_rows",
     "fftconv_workspace_bytes_linear_i8", "fftconv_linear_i8", "fftconv_act_pack", "fftconv_act_unpack",
     "fftconv_workspace_bytes_linear_grad_weight", "fftconv_linear_grad_weight",
+    "fftconv_workspace_bytes_gated_scan", "fftconv_gated_scan", "fftconv_gated_scan_backward", "fftconv_gated_step",
 ]
 
 STATIC_WORKSPACE_BYTES = 64 << 20      # FFTCONV_STATIC_WORKSPACE_BYTES
@@ -138,6 +139,10 @@ def load(path: str | None = None):
         ("fftconv_act_unpack", ci, [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, vp]),
         ("fftconv_workspace_bytes_linear_grad_weight", size, [i64, i64, i64, i64, ci, ci]),
         ("fftconv_linear_grad_weight", ci, [vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, ci, vp, vp]),
+        ("fftconv_workspace_bytes_gated_scan", size, [i64, i64, i64, ci]),
+        ("fftconv_gated_scan", ci, [vp] * 8 + [i64] * 3 + [ci, ci, vp, vp]),
+        ("fftconv_gated_scan_backward", ci, [vp] * 11 + [i64] * 3 + [ci, ci, vp, vp]),
+        ("fftconv_gated_step", ci, [vp] * 6 + [i64, ci, ci, vp]),
     ):
         getattr(lib, name).argtypes, getattr(lib, name).restype = arguments, result
     lib.fftconv_last_error.argtypes = []
@@ -173,7 +178,7 @@ def _extension():
 @functools.lru_cache(maxsize=None)
 def _fastcall():
     """call() of the binding's extension, which is built first if there is none; None where it cannot be, or where what is there was built before it took
-    as many arguments as the operators around the convolutions have (call_norm came with them)."""
+    as many arguments as the operators around the convolutions have (most_arguments says how many)."""
     if not os.path.exists(_build.fastcall_path()):
         _build.try_build_fastcall()
         importlib.invalidate_caches()
@@ -181,7 +186,7 @@ def _fastcall():
         extension = _extension()
     except ImportError:
         return None
-    return extension.call if hasattr(extension, "call_norm") else None
+    return extension.call if getattr(extension, "most_arguments", 0) >= 18 else None
 
 
 @functools.lru_cache(maxsize=None)      # (of six entry points a plan: 5 of the 90 us that a plan of short rows takes)

@@ -97,7 +97,8 @@ def _ptr(t):
 def _calls(lib):
     """The entry points of a library as functions of integers, addresses and None, through the binding's extension where it can be built."""
     fast = _f._fastcall()
-    c = {name: _f._entry(lib, "fftconv_" + name) for name in ("rms_norm_backward", "linear_i8", "act_pack", "act_unpack", "linear_grad_weight")}
+    c = {name: _f._entry(lib, "fftconv_" + name) for name in ("rms_norm_backward", "linear_i8", "act_pack", "act_unpack", "linear_grad_weight",
+                                                             "gated_scan", "gated_scan_backward", "gated_step")}
     c["quantize_rows"] = lib.fftconv_quantize_rows
     if fast is None:
         c["rms_norm"] = lambda eps, *a: lib.fftconv_rms_norm(*a[:11], eps, *a[11:])
@@ -296,3 +297,94 @@ def linear_grad_weight(dy, p, layout: str = "tokens", dtype=torch.float32):
     if rc:
         _f._check(rc)
     return dw
+
+
+_GATES = {"sigmoid": 0, "log": 1}
+
+
+def _scanned(u, w, v, lengths, gate):
+    """(b, c, n), dtype, code and gate of a scan's operands."""
+    _contiguous("u", u, _IO, 3)
+    shape, dtype = u.shape, u.dtype
+    _contiguous("w", w, (dtype,), 3, shape)
+    if v is not None:
+        _contiguous("v", v, (dtype,), 3, shape)
+    if lengths is not None:
+        _contiguous("lengths", lengths, (torch.int32,), 1, shape[:1])
+    if gate not in _GATES:
+        raise ValueError("gate is \"sigmoid\" or \"log\"")
+    if shape[2] < 1 or shape[1] < 1:
+        raise ValueError("u must have one channel and one sample at least")
+    return shape, dtype, _CODE[dtype], _GATES[gate]
+
+
+def gated_scan(u, w, v=None, state=None, lengths=None, gate: str = "sigmoid", keep: bool = False):
+    """fftconv_gated_scan: (y, last), or (y, last, kept) with keep=True, of h[t] = a[t] h[t-1] + x[t] along the samples, y = v . h.
+    u, w, v: (b, c, n) fp32, fp16 or bf16. gate "sigmoid": a = sigmoid(w), x = (1 - a) u; "log": a = exp(min(w, 0)), x = u. state (b, c) fp32:
+    before the first sample (None: zeros); last (b, c): after the last one. lengths (b,) int32: the samples of each sequence, the rest is not
+    used and zero in y. kept is what gated_scan_backward takes."""
+    shape, dtype, code, kind = _scanned(u, w, v, lengths, gate)
+    b, c, n = shape
+    if state is not None:
+        _contiguous("state", state, _F32, 2, (b, c))
+    y = torch.empty_like(u)
+    last = _empty((b, c), dtype=torch.float32, device=u.device)
+    kept = _empty((b, c, -(-n // 512)), dtype=torch.float32, device=u.device) if keep else None
+    if b:
+        lib = _f.load()
+        need = _workspace(lib, "gated_scan", b, c, n, code)
+        ws = _empty(need, dtype=torch.uint8, device=u.device) if need else None
+        rc = _calls(lib).gated_scan(u.data_ptr(), w.data_ptr(), _ptr(v), _ptr(state), _ptr(lengths), y.data_ptr(), last.data_ptr(), _ptr(kept), b, c, n,
+                                    kind, code, _ptr(ws), _f._stream_ptr())
+        if rc:
+            _f._check(rc)
+    return (y, last, kept) if keep else (y, last)
+
+
+def gated_scan_backward(dy, u, w, kept, v=None, dlast=None, lengths=None, gate: str = "sigmoid"):
+    """fftconv_gated_scan_backward: (d, dstate); d (3, b, c, n), the gradients of u, w and v one after the other, (2, b, c, n) without v, so that
+    du, dw, dv = d, and what takes a projection's parts takes d. dlast (b, c) fp32: the gradient of `last` (None: zeros); dstate (b, c) fp32."""
+    shape, dtype, code, kind = _scanned(u, w, v, lengths, gate)
+    b, c, n = shape
+    _contiguous("dy", dy, (dtype,), 3, shape)
+    _contiguous("kept", kept, _F32, 3, (b, c, -(-n // 512)))
+    if dlast is not None:
+        _contiguous("dlast", dlast, _F32, 2, (b, c))
+    d = _empty((2 if v is None else 3, b, c, n), dtype=dtype, device=u.device)
+    dstate = _empty((b, c), dtype=torch.float32, device=u.device)
+    if b:
+        lib = _f.load()
+        need = _workspace(lib, "gated_scan", b, c, n, code)
+        ws = _empty(need, dtype=torch.uint8, device=u.device) if need else None
+        at, size = d.data_ptr(), dy.numel() * dy.element_size()
+        rc = _calls(lib).gated_scan_backward(dy.data_ptr(), u.data_ptr(), w.data_ptr(), _ptr(v), kept.data_ptr(), _ptr(dlast), _ptr(lengths), at,
+                                             at + size, None if v is None else at + 2 * size, dstate.data_ptr(), b, c, n, kind, code, _ptr(ws),
+                                             _f._stream_ptr())
+        if rc:
+            _f._check(rc)
+    return d, dstate
+
+
+def gated_step(u, w, state, v=None, gate: str = "sigmoid", out=None):
+    """fftconv_gated_step: y of one sample for every channel, u, w, v and state of one shape ((b, c), say). The state after it replaces `state`, or
+    goes to `out`, where both have to be kept."""
+    _contiguous("u", u, _IO)
+    shape, dtype = u.shape, u.dtype
+    _contiguous("w", w, (dtype,), None, shape)
+    if v is not None:
+        _contiguous("v", v, (dtype,), None, shape)
+    _contiguous("state", state, _F32, None, shape)
+    if out is None:
+        out = state
+    elif out is not state:
+        _contiguous("out", out, _F32, None, shape)
+    if gate not in _GATES:
+        raise ValueError("gate is \"sigmoid\" or \"log\"")
+    y = torch.empty_like(u)
+    t = y.numel()
+    if t:
+        rc = _calls(_f.load()).gated_step(u.data_ptr(), w.data_ptr(), _ptr(v), state.data_ptr(), out.data_ptr(), y.data_ptr(), t, _GATES[gate], _CODE[dtype],
+                                          _f._stream_ptr())
+        if rc:
+            _f._check(rc)
+    return y
