@@ -329,6 +329,40 @@ int fftconv_gated_scan_backward(const void *dy, const void *u, const void *w, co
 int fftconv_gated_step(const void *u, const void *w, const void *v, const float *state, float *next, void *y, int64_t T, int gate, int dtype,
                        void *stream);
 
+/* Projection in 8-bit floating point (e4m3: a sign, four bits of exponent, three behind the first; largest 448) with a scale for each block:
+ * 1 x 128 of a row, 128 x 128 of a weight; the last ones of a row or weight may be shorter.  For the tokens t = (b, n) of B sequences of N samples
+ *     y[t, o] = sum over blocks j (x_scale[j, t] w_scale[o / 128, j]) (sum over k in j of x[t, k] w[o, k]) + bias[o].
+ *   x: (B, N, K), x_scale: (ceil(K / 128), B, N), block by block; w: (O, K), w_scale: (ceil(O / 128), ceil(K / 128)), contiguous.  The product of the two
+ *   scales is rounded to fp32 (and has to stay in its range), a block's products are added in fp32 on the matrix cores, the blocks and the bias after
+ *   one another.  bias, y, parts and dtype: as in fftconv_linear_i8.  1 <= K <= 2^20; B N and O up to 2^31 - 512, B N O up to 2^42.
+ *   workspace: fftconv_workspace_bytes_linear_f8 bytes (may be NULL when that is 0).
+ * 8-bit values: q = x / s (rounded to fp32) rounded to e4m3, with s = max |x| / 448 over the block.  Where max |x| is below 2^-100, s and q are 0;
+ * where a value is not finite, s is NaN and q is 0: what is read back is NaN throughout the block.
+ * fftconv_quantize_blocks: T rows of K values at a distance of ldx; q (T, K), scale (ceil(K / 128), T).
+ * fftconv_quantize_blocks_channels: the same of rows that lie channel by channel, x: (parts, B, K / parts, N): row (b, n) holds sample n of all channels,
+ *   part after part, what a convolution or recurrence leaves for a projection, or its gradients (parts = 3) for the one before it.  q: (B, N, K).
+ * fftconv_quantize_tiles: a weight x: (O, K), rows at a distance of ldx.  q (O, K) with scale, and qt (K, O), its transpose (for the gradient of
+ *   the projection's input), with scale_t (ceil(K / 128), ceil(O / 128)): the same values.  Either pair may be NULL. */
+int fftconv_quantize_blocks(const void *x, int64_t ldx, uint8_t *q, float *scale, int64_t T, int64_t K, int dtype, void *stream);
+int fftconv_quantize_blocks_channels(const void *x, uint8_t *q, float *scale, int64_t B, int64_t N, int64_t K, int64_t parts, int dtype, void *stream);
+int fftconv_quantize_tiles(const void *x, int64_t ldx, uint8_t *q, float *scale, uint8_t *qt, float *scale_t, int64_t O, int64_t K, int dtype, void *stream);
+size_t fftconv_workspace_bytes_linear_f8(int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype);
+int fftconv_linear_f8(const uint8_t *x, const float *x_scale, const uint8_t *w, const float *w_scale, const float *bias, void *y, int64_t B, int64_t N,
+                      int64_t K, int64_t O, int64_t parts, int dtype, void *workspace, void *stream);
+
+/* The norm of all gradients together, and clipping: with norm = sqrt(sum of all squares) over `tensors` tensors of any sizes and types,
+ *     c = min(1, max_norm / (norm + eps)),   out[i] = c grads[i].
+ *   grads, out, counts, dtypes, dtypes_out: arrays in HOST memory, read before the call returns; grads[i], out[i]: contiguous, counts[i] >= 0 values
+ *   (up to 2^40; none: the addresses may be NULL), dtypes[i] their type.  out NULL: the norm alone (max_norm and eps are not used).  out[i] may be
+ *   grads[i]; apart from that nothing that is written overlaps anything else (one tensor twice in place is refused).  dtypes_out[i]: that of grads[i],
+ *   or fp32; NULL: those of grads.  Squares are added in 64 bits, c is rounded to fp32, products are rounded to their type.  In place and with
+ *   c = 1 nothing is written.  Where a gradient is NaN, norm is NaN and so is everything; where one is infinite, norm is, and c = 0.
+ *   norm: where not NULL, the norm as fp32 goes there.  norm_in: NULL, or a norm (one fp32 on the device) that is taken instead: that of several
+ *   devices' gradients, say.  workspace: fftconv_workspace_bytes_clip_grads bytes. */
+size_t fftconv_workspace_bytes_clip_grads(const int64_t *counts, int64_t tensors);
+int fftconv_clip_grads(const void *const *grads, void *const *out, const int64_t *counts, const int *dtypes, const int *dtypes_out, int64_t tensors,
+                       double max_norm, double eps, const float *norm_in, float *norm, void *workspace, void *stream);
+
 /* Fraction of k_f that a cut-off pattern zeroes (Appendix A.4): k_f is viewed
  * as an ndim-dimensional array of shape dims[0..ndim) and, in every dimension
  * i, the last cuts[i] indices are set to zero (cuts[i] = how much of that

@@ -52,7 +52,8 @@ template <typename T> __device__ __forceinline__ void gate_of(float w, bool log_
         rest = 1.f;
         return;
     }
-    const float t = exp_below_one<CLOSE>(-fabsf(w)), r = __builtin_amdgcn_rcpf(1.f + t), tr = t * r;
+    // (a state of a long memory meets thousands of gates: the reciprocal is taken to half a unit in the last place, by a step on from the instruction's)
+    const float t = exp_below_one<CLOSE>(-fabsf(w)), d = 1.f + t, r0 = __builtin_amdgcn_rcpf(d), r = fmaf(fmaf(-d, r0, 1.f), r0, r0), tr = t * r;
     a = w >= 0.f ? r : tr;
     rest = w >= 0.f ? tr : r;
 }

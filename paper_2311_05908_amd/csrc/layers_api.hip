@@ -10,6 +10,8 @@ constexpr int64_t MOST_ROWS = MOST + 1 - 512;      // of a projection's operands
 constexpr int64_t MOST_OUT = (int64_t)1 << 42;     // values of a projection's result, so that its tiles are a number of 32 bits
 constexpr int64_t MOST_DW = (int64_t)1 << 36;      // values of a weight's gradient
 constexpr int64_t MOST_K = 131071;                 // sums of so many products of 8-bit numbers fit 32 bits
+constexpr int64_t MOST_K_F8 = (int64_t)1 << 20;    // (places within a tile's 256 rows are 32-bit numbers)
+constexpr int64_t MOST_COUNT = (int64_t)1 << 40;   // values of a gradient
 
 int bad(const char *who, const char *what)
 {
@@ -48,7 +50,7 @@ int check_acts(const char *who, int64_t B, int64_t C, int64_t N, int dtype)
     return FFTCONV_OK;
 }
 
-int check_linear(const char *who, int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype)
+int check_linear(const char *who, int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype, int64_t most_k, const char *why_k)
 {
     if (!known(dtype)) return bad(who, "unknown dtype");
     if (B < 0 || N < 1 || K < 1 || O < 1 || times(B, N, MOST_ROWS) < 0 || O > MOST_ROWS)
@@ -58,11 +60,19 @@ int check_linear(const char *who, int64_t B, int64_t N, int64_t K, int64_t O, in
         set_error("%s: B N O=%lld x %lld values of y: up to 2^42 are supported", who, (long long)(B * N), (long long)O);
         return FFTCONV_EUNSUPPORTED;
     }
-    if (K > MOST_K) {
-        set_error("%s: sums of K=%lld products may leave 32 bits: up to %lld are supported", who, (long long)K, (long long)MOST_K);
+    if (K > most_k) {
+        set_error("%s: %s=%lld%s: up to %lld are supported", who, why_k, (long long)K, most_k == MOST_K ? " products may leave 32 bits" : "", (long long)most_k);
         return FFTCONV_EUNSUPPORTED;
     }
     return FFTCONV_OK;
+}
+int check_i8(const char *who, int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype)
+{
+    return check_linear(who, B, N, K, O, parts, dtype, MOST_K, "sums of K");
+}
+int check_f8(const char *who, int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype)
+{
+    return check_linear(who, B, N, K, O, parts, dtype, MOST_K_F8, "rows of K");
 }
 
 int check_weight(const char *who, int64_t B, int64_t N, int64_t O, int64_t C, int dtype)
@@ -139,7 +149,7 @@ int fftconv_rms_norm_backward(const void *dy, int64_t lddy, const void *h, const
 
 size_t fftconv_workspace_bytes_linear_i8(int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype)
 {
-    if (B < 1 || check_linear("fftconv_workspace_bytes_linear_i8", B, N, K, O, parts, dtype) != FFTCONV_OK) return 0;
+    if (B < 1 || check_i8("fftconv_workspace_bytes_linear_i8", B, N, K, O, parts, dtype) != FFTCONV_OK) return 0;
     return lay::linear_i8_workspace(B * N, K, O);
 }
 
@@ -147,7 +157,7 @@ int fftconv_linear_i8(const int8_t *x, const float *x_scale, const int8_t *w, co
                       int64_t N, int64_t K, int64_t O, int64_t parts, int dtype, void *workspace, void *stream)
 {
     const char *const who = "fftconv_linear_i8";
-    FC_TRY(check_linear(who, B, N, K, O, parts, dtype));
+    FC_TRY(check_i8(who, B, N, K, O, parts, dtype));
     if (B == 0) return FFTCONV_OK;
     if (!x || !x_scale || !w || !w_scale || !y) return bad(who, "a tensor is NULL");
     if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4) || !aligned(workspace, 4) || !aligned(y, size_of(dtype)))
@@ -247,6 +257,105 @@ int fftconv_gated_step(const void *u, const void *w, const void *v, const float 
     if (!aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(y, to) || !aligned(state, 4) || !aligned(next, 4))
         return bad(who, "a tensor is not aligned to its elements");
     return lay::gated_step(u, w, v, state, next, y, T, gate, dtype, (hipStream_t)stream);
+}
+
+int fftconv_quantize_blocks(const void *x, int64_t ldx, uint8_t *q, float *scale, int64_t T, int64_t K, int dtype, void *stream)
+{
+    const char *const who = "fftconv_quantize_blocks";
+    if (!known(dtype)) return bad(who, "unknown dtype");
+    if (T < 0 || T > MOST || K < 1) return bad(who, "T >= 0 and K >= 1 are wanted, T below 2^31");
+    if (K > MOST_K_F8) {
+        set_error("%s: rows of K=%lld: up to %lld are supported", who, (long long)K, (long long)MOST_K_F8);
+        return FFTCONV_EUNSUPPORTED;
+    }
+    if (ldx < K || ldx > INT64_MAX / 64 / MOST) return bad(who, "the distance of rows is below K, or too large");
+    if (T == 0) return FFTCONV_OK;
+    if (!x || !q || !scale) return bad(who, "a tensor is NULL");
+    if (!aligned(x, size_of(dtype)) || !aligned(scale, 4)) return bad(who, "a tensor is not aligned to its elements");
+    return lay::quantize_blocks(x, ldx, q, scale, T, K, dtype, (hipStream_t)stream);
+}
+
+int fftconv_quantize_blocks_channels(const void *x, uint8_t *q, float *scale, int64_t B, int64_t N, int64_t K, int64_t parts, int dtype, void *stream)
+{
+    const char *const who = "fftconv_quantize_blocks_channels";
+    if (!known(dtype)) return bad(who, "unknown dtype");
+    if (B < 0 || N < 1 || K < 1 || times(B, N) < 0) return bad(who, "B >= 0, N >= 1 and K >= 1 are wanted, B N below 2^31");
+    if (parts < 1 || K % parts != 0) return bad(who, "parts has to divide K");
+    if (K > MOST_K_F8) {
+        set_error("%s: rows of K=%lld: up to %lld are supported", who, (long long)K, (long long)MOST_K_F8);
+        return FFTCONV_EUNSUPPORTED;
+    }
+    if (B == 0) return FFTCONV_OK;
+    if (!x || !q || !scale) return bad(who, "a tensor is NULL");
+    if (!aligned(x, size_of(dtype)) || !aligned(scale, 4)) return bad(who, "a tensor is not aligned to its elements");
+    return lay::quantize_blocks_channels(x, q, scale, B, N, K, parts, dtype, (hipStream_t)stream);
+}
+
+int fftconv_quantize_tiles(const void *x, int64_t ldx, uint8_t *q, float *scale, uint8_t *qt, float *scale_t, int64_t O, int64_t K, int dtype, void *stream)
+{
+    const char *const who = "fftconv_quantize_tiles";
+    if (!known(dtype)) return bad(who, "unknown dtype");
+    if (O < 1 || K < 1 || O > MOST || K > MOST) return bad(who, "O, K >= 1 are wanted, below 2^31");
+    if (ldx < K || times(O, ldx, INT64_MAX / 64) < 0) return bad(who, "the distance of rows is below K, or too large");
+    if (!x || (!q && !qt)) return bad(who, "a tensor is NULL");
+    if ((q != nullptr) != (scale != nullptr) || (qt != nullptr) != (scale_t != nullptr)) return bad(who, "8-bit values go with their scales");
+    if (!aligned(x, size_of(dtype)) || !aligned(scale, 4) || !aligned(scale_t, 4)) return bad(who, "a tensor is not aligned to its elements");
+    return lay::quantize_tiles(x, ldx, q, scale, qt, scale_t, O, K, dtype, (hipStream_t)stream);
+}
+
+size_t fftconv_workspace_bytes_linear_f8(int64_t B, int64_t N, int64_t K, int64_t O, int64_t parts, int dtype)
+{
+    if (B < 1 || check_f8("fftconv_workspace_bytes_linear_f8", B, N, K, O, parts, dtype) != FFTCONV_OK) return 0;
+    return lay::linear_f8_workspace(B * N, K, O);
+}
+
+int fftconv_linear_f8(const uint8_t *x, const float *x_scale, const uint8_t *w, const float *w_scale, const float *bias, void *y, int64_t B, int64_t N,
+                      int64_t K, int64_t O, int64_t parts, int dtype, void *workspace, void *stream)
+{
+    const char *const who = "fftconv_linear_f8";
+    FC_TRY(check_f8(who, B, N, K, O, parts, dtype));
+    if (B == 0) return FFTCONV_OK;
+    if (!x || !x_scale || !w || !w_scale || !y) return bad(who, "a tensor is NULL");
+    if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4) || !aligned(workspace, 4) || !aligned(y, size_of(dtype)))
+        return bad(who, "a tensor is not aligned to its elements");
+    if (!workspace && fftconv_workspace_bytes_linear_f8(B, N, K, O, parts, dtype) != 0) return bad(who, "the workspace is NULL");
+    return lay::linear_f8(x, x_scale, w, w_scale, bias, y, B, N, K, O, parts, dtype, workspace, (hipStream_t)stream);
+}
+
+size_t fftconv_workspace_bytes_clip_grads(const int64_t *counts, int64_t tensors)
+{
+    if (tensors < 0 || (tensors > 0 && !counts)) return 0;
+    for (int64_t i = 0; i < tensors; ++i)
+        if (counts[i] < 0 || counts[i] > MOST_COUNT) return 0;
+    return lay::clip_workspace(counts, tensors);
+}
+
+int fftconv_clip_grads(const void *const *grads, void *const *out, const int64_t *counts, const int *dtypes, const int *dtypes_out, int64_t tensors,
+                       double max_norm, double eps, const float *norm_in, float *norm, void *workspace, void *stream)
+{
+    const char *const who = "fftconv_clip_grads";
+    if (tensors < 0 || (tensors > 0 && (!grads || !counts || !dtypes))) return bad(who, "an array is NULL, or the number of tensors below 0");
+    if (!norm_in && !workspace) return bad(who, "the workspace is NULL");
+    if (!out && norm_in) return bad(who, "nothing to do: a norm is given, and no tensors to write");
+    if (!aligned(norm, 4) || !aligned(norm_in, 4) || !aligned(workspace, 8)) return bad(who, "a tensor is not aligned to its elements");
+    if (out && (!(max_norm >= 0.0) || !(eps >= 0.0) || (max_norm == 0.0 && eps == 0.0))) return bad(who, "max_norm and eps have to be numbers >= 0, one of them above");
+    const int *const types_out = dtypes_out ? dtypes_out : dtypes;
+    for (int64_t i = 0; i < tensors; ++i) {
+        if (!known(dtypes[i])) return bad(who, "unknown dtype");
+        if (counts[i] < 0 || counts[i] > MOST_COUNT) return bad(who, "a tensor has 0 to 2^40 values");
+        if (out && types_out[i] != dtypes[i] && types_out[i] != FFTCONV_F32) return bad(who, "results are in the type of the gradient or in fp32");
+        if (counts[i] > 0 && (!grads[i] || (out && !out[i]))) return bad(who, "a tensor is NULL");
+        if (!aligned(grads[i], size_of(dtypes[i])) || (out && !aligned(out[i], size_of(types_out[i])))) return bad(who, "a tensor is not aligned to its elements");
+    }
+    if (out) {
+        const int found = lay::clip_overlaps(grads, out, counts, dtypes, types_out, tensors);
+        if (found < 0) {
+            set_error("%s: no memory", who);
+            return FFTCONV_ENOMEM;
+        }
+        if (found) return bad(who, "a tensor that is written overlaps another one");
+    }
+    return lay::clip_grads(grads, out, counts, dtypes, types_out, tensors, max_norm, eps, norm_in, norm, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -43,5 +43,21 @@ int gated_scan_backward(const void *dy, const void *u, const void *w, const void
                         hipStream_t s);
 int gated_step(const void *u, const void *w, const void *v, const float *state, float *next, void *y, int64_t T, int gate, int dtype, hipStream_t s);
 
+// block_scale.hip
+int quantize_blocks(const void *x, int64_t ldx, uint8_t *q, float *scale, int64_t T, int64_t K, int dtype, hipStream_t s);
+int quantize_blocks_channels(const void *x, uint8_t *q, float *scale, int64_t B, int64_t N, int64_t K, int64_t parts, int dtype, hipStream_t s);
+int quantize_tiles(const void *x, int64_t ldx, uint8_t *q, float *scale, uint8_t *qt, float *scale_t, int64_t O, int64_t K, int dtype, hipStream_t s);
+
+// linear_f8.hip
+size_t linear_f8_workspace(int64_t T, int64_t K, int64_t O);
+int linear_f8(const uint8_t *x, const float *xs, const uint8_t *w, const float *ws, const float *bias, void *y, int64_t B, int64_t N, int64_t K,
+              int64_t O, int64_t parts, int dtype, void *workspace, hipStream_t s);
+
+// grad_clip.hip
+size_t clip_workspace(const int64_t *counts, int64_t tensors);
+int clip_overlaps(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors);
+int clip_grads(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors, double limit,
+               double eps, const float *norm_in, float *norm, void *workspace, hipStream_t s);
+
 }  // namespace lay
 }  // namespace fftconv

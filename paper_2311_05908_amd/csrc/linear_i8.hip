@@ -11,8 +11,8 @@
 // where there are 64 or less and k is about 1000 or more. Everything else is k_linear's, which takes any k at any alignment, on up to 128 x 256 (4097 x
 // 4097 -> 4097: 0.72 POP/s, where 4096 x 4096 -> 4096 makes 2.1): among it calls of 65 to 127 tiles of 128 x 128, or of fewer with a shorter k, on 64 x 64.
 // That last line has not been measured out: 4096 -> 4096 takes 20 us for 256 tokens (ranges), 39 for 257 to 384 (k_linear) and 19 for 385.
-#include "async_lds.h"
 #include "layers_index.h"
+#include "linear_common.h"
 
 namespace fftconv {
 namespace lay {
@@ -33,15 +33,6 @@ struct LinArgs {
     int ranges, per;              // of k, whose sums of a tile are added up by a second kernel (1: all of k); steps of one
     int *part;                    // (ranges, ns, nr)
 };
-
-// x / d for 0 <= x < 2^31 from the reciprocal: at most one too large before the correction.
-__device__ __forceinline__ int quotient(int x, int d, uint32_t by_d)
-{
-    if (d == 1) return x;
-    const uint32_t q = __umulhi((uint32_t)x, by_d);
-    return (int)(q - (q * (uint32_t)d > (uint32_t)x ? 1 : 0));
-}
-static uint32_t reciprocal(int64_t d) { return d > 1 ? (uint32_t)((((int64_t)1 << 32) + d - 1) / d) : 0; }
 
 // First value of y in row s of S: y[column(s) + offset(r)].
 __device__ __forceinline__ int64_t column_of(const LinArgs &a, int s)
@@ -65,22 +56,6 @@ template <int FR, int FS> struct Tile {
 // The place in LDS of 16-byte piece c (0 .. 3) of a 64-byte row. A clock delivers 256 bytes, here the same piece of sixteen rows in a run: four rows
 // lie in 256 bytes, so the piece is moved by the row's number above that, and all sixteen come from banks of their own.
 __device__ __forceinline__ int piece_at(int row, int c) { return row * 64 + ((c ^ ((row >> 2) & 3)) << 4); }
-
-// 16 bytes of a row of K from column k on; what lies beyond K reads as zero.
-__device__ __forceinline__ uint4 load16(const int8_t *row, int64_t k, int64_t K)
-{
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (k + 16 <= K) {
-        __builtin_memcpy(&v, row + k, 16);
-    } else if (k < K) {
-        uint32_t w[4] = {};
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if (k + e < K) w[e / 4] |= (uint32_t)(uint8_t)row[k + e] << (8 * (e % 4));
-        v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    return v;
-}
 
 __device__ __forceinline__ i32x16 mfma_i8(uint4 a, uint4 b, i32x16 c)
 {
@@ -167,15 +142,6 @@ template <typename T, bool CHANNELS> __device__ __forceinline__ void scaled_to_l
             *(uint2 *)(own + l32 * 128 + (((4 * part + q) ^ ((l32 >> 1) & 7)) << 4) + ((half ^ (l32 >> 4)) << 3)) = w;
         }
     }
-}
-// 16 bytes to y. Past the caches where y would only push everything else out of the memory-side one: bf16 64 x 4096 x 768 -> 3 x 768, 1.2 GB, 643 -> 619 us;
-// f16 8192 x 4096 -> 16384, 0.27 GB, 505 us with and 512 without them.
-template <bool BEYOND> __device__ __forceinline__ void put16(char *to, uint4 v)
-{
-    typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4;
-    const u32x4 w = {v.x, v.y, v.z, v.w};
-    if constexpr (BEYOND) __builtin_nontemporal_store(w, (u32x4 *)to);
-    else *(u32x4 *)to = w;
 }
 // Piece (lane % 8) of column lane / 8 + 8 t of what lies there.
 template <typename T> __device__ __forceinline__ uint4 column_piece(const char *own, int t)
@@ -267,18 +233,6 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) 
 // and stored (150) comes on top rather than beside them, for results are written after a tile's products; without any wait for a transfer, or
 // without barriers, the time is the same. Hence the large tile (128 x 128: 741 and 917 us), whole lines to a store, and places in y that cost
 // no arithmetic.
-//
-// Which tile: workgroups go to the dies in turn; a die takes a stretch of the tiles, its workgroups side by side, in an order in which
-// neighbours share rows of R or of S, so that those come from its L2.
-struct Walk {
-    int tiles_s, group, tiles;
-    __device__ __forceinline__ void place(int i, int &tr, int &ts, int tiles_r) const
-    {
-        const int whole = tiles_r * group, g = i / whole, k = i - g * whole, width = min(group, tiles_s - g * group);
-        tr = k / width, ts = g * group + (k - tr * width);
-    }
-};
-
 template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void __launch_bounds__(512, 2) k_linear_async(const LinArgs a, const Walk walk)
 {
     constexpr int BR = 64 * FR, BS = 128 * FS, BK = 64, STAGE = (BR + BS) * BK, STAGES = 4, LI = (BR + BS) / 128;

@@ -32,6 +32,8 @@ EXPORTS = [
     "fftconv_workspace_bytes_linear_i8", "fftconv_linear_i8", "fftconv_act_pack", "fftconv_act_unpack",
     "fftconv_workspace_bytes_linear_grad_weight", "fftconv_linear_grad_weight",
     "fftconv_workspace_bytes_gated_scan", "fftconv_gated_scan", "fftconv_gated_scan_backward", "fftconv_gated_step",
+    "fftconv_quantize_blocks", "fftconv_quantize_blocks_channels", "fftconv_quantize_tiles", "fftconv_workspace_bytes_linear_f8", "fftconv_linear_f8",
+    "fftconv_workspace_bytes_clip_grads", "fftconv_clip_grads",
 ]
 
 STATIC_WORKSPACE_BYTES = 64 << 20      # FFTCONV_STATIC_WORKSPACE_BYTES
@@ -143,6 +145,13 @@ def load(path: str | None = None):
         ("fftconv_gated_scan", ci, [vp] * 8 + [i64] * 3 + [ci, ci, vp, vp]),
         ("fftconv_gated_scan_backward", ci, [vp] * 11 + [i64] * 3 + [ci, ci, vp, vp]),
         ("fftconv_gated_step", ci, [vp] * 6 + [i64, ci, ci, vp]),
+        ("fftconv_quantize_blocks", ci, [vp, i64, vp, vp, i64, i64, ci, vp]),
+        ("fftconv_quantize_blocks_channels", ci, [vp, vp, vp, i64, i64, i64, i64, ci, vp]),
+        ("fftconv_quantize_tiles", ci, [vp, i64, vp, vp, vp, vp, i64, i64, ci, vp]),
+        ("fftconv_workspace_bytes_linear_f8", size, [i64, i64, i64, i64, i64, ci]),
+        ("fftconv_linear_f8", ci, [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, ci, vp, vp]),
+        ("fftconv_workspace_bytes_clip_grads", size, [vp, i64]),
+        ("fftconv_clip_grads", ci, [vp, vp, vp, vp, vp, i64, dbl, dbl, vp, vp, vp, vp]),
     ):
         getattr(lib, name).argtypes, getattr(lib, name).restype = arguments, result
     lib.fftconv_last_error.argtypes = []

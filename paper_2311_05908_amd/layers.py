@@ -10,6 +10,7 @@ device; PyTorch supplies memory. Tensors that are not laid out as a call wants t
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 from typing import NamedTuple
@@ -36,7 +37,28 @@ class Checkpoint8(NamedTuple):
     scale: torch.Tensor
 
 
+class Blocks8(NamedTuple):
+    """Rows in 8-bit floating point: q (..., k) e4m3 and scale (ceil(k / 128), ...) fp32, block by block: scale[j, i] is that of q[i, 128 j : 128 (j + 1)]."""
+    q: torch.Tensor
+    scale: torch.Tensor
+
+    def float(self):
+        k = self.q.shape[-1]
+        return self.q.float() * self.scale.movedim(0, -1).repeat_interleave(128, -1)[..., :k]
+
+
+class Tiles8(NamedTuple):
+    """A weight in 8-bit floating point: q (o, k) e4m3 and scale (ceil(o / 128), ceil(k / 128)) fp32, one for 128 x 128."""
+    q: torch.Tensor
+    scale: torch.Tensor
+
+    def float(self):
+        o, k = self.q.shape
+        return self.q.float() * self.scale.repeat_interleave(128, 0)[:o].repeat_interleave(128, 1)[:, :k]
+
+
 _IO = tuple(_f._DTYPE_CODE)
+_F8 = torch.float8_e4m3fn
 _F32, _I8 = (torch.float32,), (torch.int8,)
 _CODE = _f._DTYPE_CODE
 _device = _f._current_device
@@ -98,8 +120,9 @@ def _calls(lib):
     """The entry points of a library as functions of integers, addresses and None, through the binding's extension where it can be built."""
     fast = _f._fastcall()
     c = {name: _f._entry(lib, "fftconv_" + name) for name in ("rms_norm_backward", "linear_i8", "act_pack", "act_unpack", "linear_grad_weight",
-                                                             "gated_scan", "gated_scan_backward", "gated_step")}
-    c["quantize_rows"] = lib.fftconv_quantize_rows
+                                                             "gated_scan", "gated_scan_backward", "gated_step", "quantize_blocks_channels",
+                                                             "quantize_tiles", "linear_f8")}
+    c["quantize_rows"], c["quantize_blocks"] = lib.fftconv_quantize_rows, lib.fftconv_quantize_blocks
     if fast is None:
         c["rms_norm"] = lambda eps, *a: lib.fftconv_rms_norm(*a[:11], eps, *a[11:])
     else:
@@ -388,3 +411,141 @@ def gated_step(u, w, state, v=None, gate: str = "sigmoid", out=None):
         if rc:
             _f._check(rc)
     return y
+
+
+def quantize_blocks(x, layout: str = "tokens", parts: int = 1):
+    """fftconv_quantize_blocks: rows x (..., k) in e4m3 with a scale for each 128 of them (Blocks8), what linear_f8 takes. layout "channels":
+    fftconv_quantize_blocks_channels, of x (b, k, n), or (parts, b, k / parts, n) with parts > 1; q is (b, n, k) either way."""
+    if layout == "tokens" and parts == 1:
+        t, k, ldx = _rows("x", x)
+        shape, dtype, device = x.shape, x.dtype, x.device
+        q = _empty(shape, dtype=_F8, device=device)
+        scale = _empty((-(-k // 128), *shape[:-1]), dtype=torch.float32, device=device)
+        if t:
+            rc = _calls(_f.load()).quantize_blocks(x.data_ptr(), ldx, q.data_ptr(), scale.data_ptr(), t, k, _CODE[dtype], _f._stream_ptr())
+            if rc:
+                _f._check(rc)
+        return Blocks8(q, scale)
+    parts = int(parts)
+    if layout != "channels" or parts < 1:
+        raise ValueError("layout is \"tokens\" or \"channels\", parts 1 for tokens")
+    _contiguous("x", x, _IO, 4 if parts > 1 else 3)
+    if parts > 1 and x.shape[0] != parts:
+        raise ValueError("x must be (parts, b, channels, n)")
+    b, c, n = x.shape[-3:]
+    k = parts * c
+    if k < 1 or n < 1:
+        raise ValueError("x must have one channel and one sample at least")
+    q = _empty((b, n, k), dtype=_F8, device=x.device)
+    scale = _empty((-(-k // 128), b, n), dtype=torch.float32, device=x.device)
+    if b:
+        rc = _calls(_f.load()).quantize_blocks_channels(x.data_ptr(), q.data_ptr(), scale.data_ptr(), b, n, k, parts, _CODE[x.dtype], _f._stream_ptr())
+        if rc:
+            _f._check(rc)
+    return Blocks8(q, scale)
+
+
+def quantize_tiles(w, transposed: bool = False):
+    """fftconv_quantize_tiles: a weight (o, k) in e4m3 with a scale for each 128 x 128 (Tiles8), once for every call until it changes. With transposed=True
+    a pair, the second one of w^T (k, o), the same values: what the gradient of the projection's input is multiplied with."""
+    o, k, ldw = _rows("w", w)
+    if w.dim() != 2 or o < 1:
+        raise ValueError("w must be (o, k), one output at least")
+    to, tk, device = -(-o // 128), -(-k // 128), w.device
+    q, scale = _empty((o, k), dtype=_F8, device=device), _empty((to, tk), dtype=torch.float32, device=device)
+    qt = scale_t = None
+    if transposed:
+        qt, scale_t = _empty((k, o), dtype=_F8, device=device), _empty((tk, to), dtype=torch.float32, device=device)
+    rc = _calls(_f.load()).quantize_tiles(w.data_ptr(), ldw, q.data_ptr(), scale.data_ptr(), _ptr(qt), _ptr(scale_t), o, k, _CODE[w.dtype], _f._stream_ptr())
+    if rc:
+        _f._check(rc)
+    return (Tiles8(q, scale), Tiles8(qt, scale_t)) if transposed else Tiles8(q, scale)
+
+
+def linear_f8(rows, weight, bias=None, dtype=torch.bfloat16, layout: str = "tokens", parts: int = 1):
+    """fftconv_linear_f8: rows (b, n, k) (or (t, k): one sequence), Blocks8 or a pair (q, scale), and weight (o, k), Tiles8 or a pair; bias (o,) fp32.
+    layout "tokens": y (b, n, o). "channels": y (b, o, n), or (parts, b, o / parts, n) with parts > 1."""
+    (xq, xs), (wq, ws) = rows, weight
+    _contiguous("rows", xq, (_F8,))
+    if xq.dim() not in (2, 3):
+        raise ValueError("rows must be (b, n, k) or (t, k)")
+    _contiguous("weight", wq, (_F8,), 2)
+    o, k = wq.shape
+    if xq.shape[-1] != k or k < 1 or o < 1:
+        raise ValueError("rows and weight differ in length, or have none")
+    blocks = -(-k // 128)
+    _contiguous("the rows' scale", xs, _F32, None, (blocks, *xq.shape[:-1]))
+    _contiguous("the weight's scale", ws, _F32, None, (-(-o // 128), blocks))
+    if bias is not None:
+        _contiguous("bias", bias, _F32, 1, (o,))
+    if dtype not in _CODE:
+        raise ValueError("dtype must be fp32, fp16 or bf16")
+    parts = int(parts)
+    if layout not in ("tokens", "channels") or parts < 1 or (layout == "tokens" and parts != 1) or o % parts:
+        raise ValueError("layout is \"tokens\" or \"channels\", parts a divisor of the output channels (1 for tokens)")
+    b, n = (1, xq.shape[0]) if xq.dim() == 2 else xq.shape[:2]
+    if layout == "tokens":
+        shape = (*xq.shape[:-1], o)
+    else:
+        shape = (parts, b, o // parts, n) if parts > 1 else (b, o, n)
+        shape = shape if xq.dim() == 3 else shape[:-3] + shape[-2:]
+    y = _empty(shape, dtype=dtype, device=xq.device)
+    if y.numel() == 0:
+        return y
+    p, code, lib = 0 if layout == "tokens" else parts, _CODE[dtype], _f.load()
+    need = _workspace(lib, "linear_f8", b, n, k, o, p, code)
+    work = _empty(need, dtype=torch.uint8, device=xq.device) if need else None
+    rc = _calls(lib).linear_f8(xq.data_ptr(), xs.data_ptr(), wq.data_ptr(), ws.data_ptr(), _ptr(bias), y.data_ptr(), b, n, k, o, p, code, _ptr(work),
+                               _f._stream_ptr())
+    if rc:
+        _f._check(rc)
+    return y
+
+
+def _clip(grads, max_norm, out, norm, eps, write):
+    grads = list(grads)
+    for t in grads:
+        _contiguous("a gradient", t, _IO)
+    device = torch.device("cuda", _device())
+    counts = array.array("q", [t.numel() for t in grads])
+    types = array.array("i", [_CODE[t.dtype] for t in grads])
+    at = array.array("Q", [t.data_ptr() for t in grads])
+    to, types_to, result = None, None, norm
+    if write:
+        to, types_to = at, types
+        if out is not None:
+            out = list(out)
+            if len(out) != len(grads):
+                raise ValueError("out must have a tensor for each gradient")
+            for t, o in zip(grads, out):
+                _contiguous("a tensor of out", o, (t.dtype, torch.float32), None, t.shape)
+            to = array.array("Q", [t.data_ptr() for t in out])
+            types_to = array.array("i", [_CODE[t.dtype] for t in out])
+        if norm is not None:
+            _contiguous("norm", norm, _F32)
+            if norm.numel() != 1:
+                raise ValueError("norm must be one number")
+        if not grads and norm is not None:
+            return norm
+    lib, work, n = _f.load(), None, len(grads)
+    address = lambda a: a.buffer_info()[0] if a else None  # noqa: E731
+    if norm is None:
+        result = _empty((), dtype=torch.float32, device=device)
+        work = _empty(lib.fftconv_workspace_bytes_clip_grads(address(counts), n), dtype=torch.uint8, device=device)
+    rc = lib.fftconv_clip_grads(address(at), address(to), address(counts), address(types), address(types_to), n, max_norm, eps, _ptr(norm),
+                                None if norm is not None else result.data_ptr(), _ptr(work), _f._stream_ptr())
+    if rc:
+        _f._check(rc)
+    return result
+
+
+def grad_norm(grads):
+    """fftconv_clip_grads without clipping: the 2-norm over all of the tensors together, () fp32 on the device. grads: any number of contiguous
+    tensors of any sizes, each fp32, fp16 or bf16; squares are added in 64 bits."""
+    return _clip(grads, 0.0, None, None, 0.0, False)
+
+
+def clip_grads(grads, max_norm: float, out=None, norm=None, eps: float = 1e-6):
+    """fftconv_clip_grads: every gradient times min(1, max_norm / (norm + eps)), in place, or into `out`, a tensor for each of the same shape and type or
+    in fp32. norm: what grad_norm gave, or the norm over other devices' gradients too, one fp32 on the device; None: that of grads. Returns the norm."""
+    return _clip(grads, float(max_norm), out, norm, float(eps), True)

@@ -1,0 +1,336 @@
+"""8-bit floating point with scales of blocks, and the projections from it, on the GPU against their definitions in 64 bits.
+
+Quantised values are compared bit for bit: the quotient as fp32 rounds it (of 64-bit quotients, whose own rounding cannot change that of fp32
+numbers), rounded to e4m3. Products: the scales' product is rounded (E = 2^-24), a block's sum of 128 products of 8-bit numbers in fp32, in whatever
+order, is within 128 E of the sum of their magnitudes, multiply-add and total over the blocks within (blocks + 1) E of it, the sum with the bias E;
+then the result is rounded to its type (U). Where results are in 16 bits, the matrix cores' products of e4m3 are taken: of eight neighbours along k seven
+may lose what is below 2^-13 of the largest, 7 2^-13 of the sum of all magnitudes at most (each eight's largest is no more than their sum)."""
+import pytest
+import torch
+
+from paper_2311_05908_amd import layers
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+U = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 0.0, "f16": 2.0 ** -25, "bf16": 0.0}
+E = 2.0 ** -24
+F8 = torch.float8_e4m3fn
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, *shape, dtype=torch.float32):
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def e4m3(x):
+    """fp32 numbers rounded to those of e4m3, ties to even: steps of 2^(exponent - 3), 2^-9 at least."""
+    x = x.double()
+    step = torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=2.0 ** -30))).clamp(min=-6) - 3)
+    return torch.round(x / step) * step
+
+
+def scale_of(top):
+    s = torch.where(top < 2.0 ** -100, torch.zeros_like(top), (top.double() / 448).float())
+    return torch.where(torch.isfinite(top), s, torch.full_like(s, float("nan")))
+
+
+def quantised(x, s):
+    """x with the scale of every value's block"""
+    q = e4m3((x.double() / torch.where(s > 0, s, torch.ones_like(s)).double()).float())
+    return torch.where(s > 0, q, torch.zeros_like(q))
+
+
+def blocks8(x):
+    """(q as 64-bit numbers, scale (blocks, ...)) of rows."""
+    k = x.shape[-1]
+    n = -(-k // 128)
+    s = scale_of(torch.nn.functional.pad(x.float(), (0, n * 128 - k)).unflatten(-1, (n, 128)).abs().amax(-1))
+    return quantised(x.float(), s.repeat_interleave(128, -1)[..., :k]), s.movedim(-1, 0)
+
+
+def tiles8(w):
+    o, k = w.shape
+    to, tk = -(-o // 128), -(-k // 128)
+    s = scale_of(torch.nn.functional.pad(w.float(), (0, tk * 128 - k, 0, to * 128 - o)).reshape(to, 128, tk, 128).abs().amax((1, 3)))
+    return quantised(w.float(), s.repeat_interleave(128, 0)[:o].repeat_interleave(128, 1)[:, :k]), s
+
+
+def same(got, ref):
+    (q, s), (rq, rs) = got, ref
+    assert q.dtype == F8 and q.shape == rq.shape and s.shape == rs.shape and s.is_contiguous()
+    assert torch.equal(torch.nan_to_num(s, nan=-1.0), torch.nan_to_num(rs.contiguous(), nan=-1.0))
+    assert torch.equal(q.double(), rq), "%d of %d places" % (int((q.double() != rq).sum()), rq.numel())
+
+
+ROWS = [(1, 1), (1, 128), (3, 127), (2, 129), (5, 1000), (1, 4096), (16, 768), (17, 769), (100, 255), (1000, 640), (33, 5000)]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t,k", ROWS)
+def test_blocks_of_rows(t, k, dtype):
+    g = gen(t * 7 + k)
+    x = normal(g, t, k, dtype=DT[dtype]) * torch.exp2(torch.randint(-30 if dtype != "f16" else -8, 8, (t, k), generator=g, device="cuda").float()).to(DT[dtype])
+    same(layers.quantize_blocks(x), blocks8(x))
+    wide = normal(g, t, k + 5, dtype=DT[dtype])
+    same(layers.quantize_blocks(wide[:, 3:k + 3]), blocks8(wide[:, 3:k + 3]))
+
+
+def test_quotients_next_to_ties():
+    """Values whose quotient is at the middle between two numbers of e4m3, or the fp32 numbers on either side, for many scales."""
+    g = gen(1)
+    t = 4096
+    top = torch.rand(t, generator=g, device="cuda") * 2 + 0.5
+    top[:64] *= torch.exp2(torch.arange(-99.0, -35.0, device="cuda"))
+    top[64:128] *= torch.exp2(torch.arange(60.0, 124.0, device="cuda"))
+    s = scale_of(top)
+    grid = e4m3(torch.arange(0, 127, device="cuda").to(torch.uint8).view(F8).float()).unique()
+    middle = ((grid[1:] + grid[:-1]) / 2)[None]
+    near = (middle * s.double()[:, None]).float()
+    for way in (near, torch.nextafter(near, torch.full_like(near, float("inf"))), torch.nextafter(near, torch.zeros_like(near))):
+        x = torch.cat([way[:, :125], top[:, None]], 1)
+        same(layers.quantize_blocks(x), blocks8(x))
+        same(layers.quantize_blocks(-x), blocks8(-x))
+
+
+def test_blocks_without_a_scale():
+    """Zeros, blocks below 2^-100, infinities and NaN: of their own block alone."""
+    x = normal(gen(2), 20, 400)
+    x[0, :128] = 0
+    x[1, 128:256] = 2.0 ** -101
+    x[2, 130] = float("inf")
+    x[3, 399] = float("nan")
+    x[4] = 3e38
+    x[5, :128] = 2.0 ** -100
+    x[6, 256:] = 0
+    q, s = layers.quantize_blocks(x)
+    same((q, s), blocks8(x))
+    assert torch.isnan(s[1, 2]) and torch.isnan(s[3, 3]) and int(torch.isnan(s).sum()) == 2
+    back = layers.Blocks8(q, s).float()
+    assert torch.isnan(back[2, 128:256]).all() and int(torch.isnan(back).sum()) == 128 + 16
+    w = x[:, :300].contiguous()
+    a, b = layers.quantize_tiles(w, transposed=True)
+    same(a, tiles8(w))
+    same(b, tiles8(w.t()))
+    c = x.t().reshape(1, 400, 20).contiguous()
+    same(layers.quantize_blocks(c, layout="channels"), blocks8(x[None]))
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("parts,b,c,n", [(1, 1, 1, 1), (1, 2, 128, 64), (3, 2, 100, 65), (1, 3, 129, 63), (3, 1, 768, 100), (2, 2, 3, 7), (1, 1, 1000, 513), (5, 3, 26, 200)])
+def test_blocks_from_channels(parts, b, c, n, dtype):
+    x = normal(gen(n + c), parts, b, c, n, dtype=DT[dtype])
+    rows = x.permute(1, 3, 0, 2).flatten(2).contiguous()
+    got = layers.quantize_blocks(x if parts > 1 else x[0], layout="channels", parts=parts)
+    same(got, blocks8(rows))
+    same(got, [t if i else t.double() for i, t in enumerate(layers.quantize_blocks(rows))])
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("o,k", [(1, 1), (128, 128), (129, 127), (7, 1000), (300, 200), (768, 769), (2304, 768)])
+def test_tiles(o, k, dtype):
+    g = gen(o + k)
+    w = normal(g, o, k, dtype=DT[dtype])
+    same(layers.quantize_tiles(w), tiles8(w))
+    a, b = layers.quantize_tiles(w, transposed=True)
+    same(a, tiles8(w))
+    same(b, tiles8(w.t()))
+    wide = normal(g, o, k + 3, dtype=DT[dtype])
+    same(layers.quantize_tiles(wide[:, 1:k + 1], transposed=True)[1], tiles8(wide[:, 1:k + 1].t()))
+
+
+def product(rows, weight, bias=None):
+    """(value, bound before the rounding) of y (..., o)"""
+    (xq, xs), (wq, ws) = rows, weight
+    o, k = wq.shape
+    x = xq.double() * xs.double().movedim(0, -1).repeat_interleave(128, -1)[..., :k]
+    w = wq.double() * ws.double().repeat_interleave(128, 0)[:o].repeat_interleave(128, 1)[:, :k]
+    lead, (x, w) = x.shape[:-1], (x.reshape(-1, k).contiguous(), w.t().contiguous())
+    y, m = x @ w, x.abs() @ w.abs()
+    bound = (128 + xs.shape[0] + 3) * E * m
+    if bias is not None:
+        y = y + bias.double()
+        bound = bound + E * (y.abs() + bias.double().abs())
+    return y.reshape(*lead, o), bound.reshape(*lead, o)
+
+
+def laid(y, parts):
+    b, n, o = y.shape
+    y = y.reshape(b, n, parts, o // parts).permute(2, 0, 3, 1)
+    return y if parts > 1 else y[0]
+
+
+def within(got, value, bound, dtype):
+    assert got.shape == value.shape
+    if dtype != "f32":
+        bound = bound * (1 + 7 * 2.0 ** -13 / (128 * E))         # (the bound has 128 E of the magnitudes and more)
+    top = {"f16": 65504.0}.get(dtype, 3e38)
+    got, value = got.double().clamp(-top, top), value.clamp(-top, top)
+    over = (got - value).abs() - (bound * (1 + U[dtype]) + U[dtype] * value.abs() + TINY[dtype])
+    assert torch.isfinite(got).all() and (over.numel() == 0 or float(over.max()) <= 0), "%g over at %d of %d places" % (
+        float(over.max()), int((over > 0).sum()), over.numel())
+
+
+def operands(g, b, n, k, o, bias=True):
+    big = 1 + 19 * (torch.rand(k, generator=g, device="cuda") < 0.02)
+    rows = layers.quantize_blocks(normal(g, b, n, k) * big)
+    weight = layers.quantize_tiles(normal(g, o, k) / k ** 0.5)
+    return rows, weight, normal(g, o) if bias else None
+
+
+SHAPES = [(1, 1, 1, 1), (1, 1, 128, 16), (1, 1, 4096, 4096), (2, 1, 129, 17), (1, 7, 1000, 33), (1, 16, 768, 300), (3, 6, 640, 129), (1, 32, 777, 48), (2, 31, 2048, 160),
+          (1, 64, 128, 768), (1, 65, 128, 64), (1, 100, 4096, 512), (1, 70, 2048, 100), (2, 128, 256, 256), (1, 200, 1000, 300), (1, 129, 16, 130), (3, 333, 272, 384),
+          (1, 1024, 768, 2304), (2, 1000, 144, 2000), (1, 2100, 528, 2050), (5, 257, 1041, 515), (1, 2048, 384, 2048), (2, 2048, 768, 4608), (4, 1111, 400, 4099)]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("b,n,k,o", SHAPES)
+def test_linear(b, n, k, o, dtype):
+    rows, weight, bias = operands(gen(k + o + n), b, n, k, o)
+    value, bound = product(rows, weight, bias)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype]), value, bound, dtype)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
+    value, bound = product(rows, weight)
+    within(layers.linear_f8(rows, weight, dtype=DT[dtype]), value, bound, dtype)
+    parts = next((p for p in (3, 2, 5) if o % p == 0), 1)
+    within(layers.linear_f8(rows, weight, dtype=DT[dtype], layout="channels", parts=parts), laid(value, parts), laid(bound, parts), dtype)
+
+
+def test_sums_are_as_fine_as_fp32():
+    """Blocks whose products cancel but for one: 448^2 = 49 2^12 and 2^-2 add up within fp32's 24 bits, so what remains is exact, where
+    products that keep 13 bits below the largest leave nothing."""
+    for t, o in ((1, 16), (100, 200), (300, 4000), (2048, 4096)):
+        k = 512
+        x, w = torch.zeros(t, k, device="cuda"), torch.zeros(o, k, device="cuda")
+        x[:, 0::128], x[:, 1::128], x[:, 2::128], w[:, 0::128], w[:, 1::128] = 448, 448, 2.0 ** -6, 448, -448
+        w[:, 2::128] = 2.0 ** 4
+        rows = layers.quantize_blocks(x)
+        weight = layers.quantize_tiles(w)
+        assert torch.equal(rows.float(), x) and torch.equal(weight.float(), w)
+        assert torch.equal(layers.linear_f8(rows, weight, dtype=torch.float32), torch.full((t, o), 4 * 2.0 ** -2, device="cuda"))
+
+
+def test_scales_of_every_size_reach_their_own():
+    """A row with NaN, a tile with NaN and scales of zero meet their own results alone."""
+    for t, k, o in ((20, 300, 300), (200, 256, 300), (200, 300, 300), (2048, 256, 4096)):
+        rows, weight, _ = operands(gen(t), 1, t, k, o)
+        clean = layers.linear_f8(rows, weight, dtype=torch.float32)
+        rows.scale[1, 0, 3] = float("nan")
+        weight.scale[2, 1] = float("nan")
+        rows.scale[0, 0, 5] = 0
+        y = layers.linear_f8(rows, weight, dtype=torch.float32)
+        bad = torch.zeros_like(y, dtype=torch.bool)
+        bad[:, 3] = True
+        bad[:, :, 256:384] = True
+        assert torch.equal(torch.isnan(y), bad)
+        rest = ~bad
+        rest[:, 5] = False
+        assert torch.equal(y[rest], clean[rest]) and not torch.equal(y[:, 5, :256], clean[:, 5, :256])
+
+
+def test_operands_at_any_byte():
+    g = gen(9)
+    rows, weight, bias = operands(g, 1, 300, 256, 384)
+    want = layers.linear_f8(rows, weight, bias=bias)
+    value, bound = product(rows, weight, bias)
+    for shift in (1, 8):
+        store = torch.empty(300 * 256 + shift, dtype=torch.uint8, device="cuda")
+        q = store[shift:].view(1, 300, 256)
+        q.copy_(rows.q.view(torch.uint8))
+        within(layers.linear_f8((q.view(F8), rows.scale), weight, bias=bias), value, bound, "bf16")
+    within(want, value, bound, "bf16")
+
+
+def test_gradient_of_the_input():
+    """dx = dy W by the transposed tiles: against the product with what the tiles stand for."""
+    g = gen(4)
+    w = normal(g, 384, 200) / 14
+    tiles, tiles_t = layers.quantize_tiles(w, transposed=True)
+    assert torch.equal(tiles.float().t(), tiles_t.float())
+    dy = normal(g, 3, 2, 128, 150, dtype=torch.bfloat16)
+    rows = layers.quantize_blocks(dy, layout="channels", parts=3)
+    value, bound = product(rows, tiles_t)
+    within(layers.linear_f8(rows, tiles_t), value, bound, "bf16")
+
+
+def test_many_rows_and_outputs():
+    """Places in results beyond 2^32 bytes, and tensors of more than 2^31 bytes."""
+    g = gen(5)
+    t, k, o = 70000, 32, 40000
+    rows, weight = layers.quantize_blocks(normal(g, t, k)), layers.quantize_tiles(normal(g, o, k))
+    y = layers.linear_f8(rows, weight)
+    few = layers.linear_f8((rows.q[-2049:].contiguous(), rows.scale[:, -2049:].contiguous()), weight)
+    value, bound = product((rows.q[-50:], rows.scale[:, -50:]), weight)
+    within(y[-50:], value, bound, "bf16")
+    within(few[-50:], value, bound, "bf16")
+    del y
+    y = layers.linear_f8(rows, weight, layout="channels")
+    within(y[:, -50:], value.t(), bound.t(), "bf16")
+
+
+def test_streams_and_graphs():
+    """Ranges of k with a workspace each: two graphs, replayed over new inputs with eager calls between."""
+    made = [operands(gen(s), 1, 100, 4096, 512) for s in range(3)]
+    want = [layers.linear_f8(r, w, bias=b, dtype=torch.float32) for r, w, b in made]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y = layers.linear_f8(made[0][0], made[0][1], bias=made[0][2], dtype=torch.float32)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(y, want[0])
+    graphs, outs, ins = [], [], []
+    for s in (0, 1):
+        x = torch.empty(1, 100, 4096, device="cuda")
+        w = [t.clone() for t in made[s][1]]
+        b = made[s][2].clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(layers.linear_f8(layers.quantize_blocks(x), w, bias=b, dtype=torch.float32))
+        graphs.append(graph)
+        ins.append((x, w, b))
+    for turn in range(4):
+        for i, (x, w, b) in enumerate(ins):
+            rows, weight, bias = made[(turn + i) % 3]
+            x.copy_(rows.float())
+            for a, c in zip(w, weight):
+                a.copy_(c)
+            b.copy_(bias)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for i, y in enumerate(outs):
+            rows, weight, bias = made[(turn + i) % 3]
+            again = layers.linear_f8(layers.quantize_blocks(rows.float()), weight, bias=bias, dtype=torch.float32)
+            assert torch.equal(y, again)
+
+
+def test_nothing_to_do():
+    x = torch.empty(0, 300, device="cuda")
+    rows = layers.quantize_blocks(x)
+    assert rows.q.shape == (0, 300) and rows.scale.shape == (3, 0)
+    weight = layers.quantize_tiles(torch.ones(5, 300, device="cuda"))
+    assert layers.linear_f8(rows, weight).shape == (0, 5)
+    assert layers.quantize_blocks(torch.empty(3, 0, 4, 7, device="cuda"), layout="channels", parts=3).q.shape == (0, 7, 12)
+
+
+def test_refusals():
+    x = torch.ones(2, 8, 256, device="cuda")
+    rows, weight = layers.quantize_blocks(x), layers.quantize_tiles(torch.ones(6, 256, device="cuda"))
+    bad = [((rows.q[:, ::2], rows.scale), weight, {}), ((rows.q, rows.scale[:1]), weight, {}), ((rows.q, rows.scale.movedim(0, -1)), weight, {}),
+           ((rows.q, rows.scale.movedim(0, -1).contiguous()), weight, {}), ((rows.q.view(torch.uint8), rows.scale), weight, {}), (rows, (weight.q[:, :128], weight.scale), {}),
+           (rows, (weight.q, weight.scale.t()), {}), (rows, weight, dict(bias=torch.ones(5, device="cuda"))), (rows, weight, dict(layout="rows")),
+           (rows, weight, dict(layout="channels", parts=4)), (rows, weight, dict(parts=2)), (rows, weight, dict(dtype=torch.float64)),
+           ((rows.q[None], rows.scale[:, None]), weight, {}), ((rows.q.cpu(), rows.scale), weight, {})]
+    for r, w, kw in bad:
+        with pytest.raises(ValueError):
+            layers.linear_f8(r, w, **kw)
+    for a, kw in ((x.int(), {}), (x.transpose(1, 2), {}), (x, dict(layout="rows")), (x, dict(parts=2)), (x, dict(layout="channels", parts=2)), (x.cpu(), {}),
+                  (x[None], dict(layout="channels", parts=3)), (x[:, :, ::2], dict(layout="channels")), (x[..., :0], {})):
+        with pytest.raises(ValueError):
+            layers.quantize_blocks(a, **kw)
+    for a in (x, x[0].t(), x[0].cpu(), x[0].double(), x[0][:, :0]):
+        with pytest.raises(ValueError):
+            layers.quantize_tiles(a)

@@ -1,0 +1,123 @@
+"""What the gated recurrence, the projections in 8-bit floating point and the gradients' clipping refuse, before any device is touched, through the C ABI."""
+import ctypes
+
+import pytest
+
+from paper_2311_05908_amd import fftconv
+
+F32, F16, BF16 = 0, 1, 2
+OK, EINVAL, EUNSUPPORTED = 0, -1, -2
+A = 4096          # an address that is aligned and never read
+
+
+def call(name, *a):
+    lib = fftconv.load()
+    rc = getattr(lib, name)(*a)
+    if rc != OK:
+        assert name in lib.fftconv_last_error().decode()
+    return rc
+
+
+def scan(u=A, w=A, v=A, state=A, lengths=A, y=A, last=A, kept=A, b=2, c=3, n=100, gate=0, dtype=BF16, ws=A):
+    return call("fftconv_gated_scan", u, w, v, state, lengths, y, last, kept, b, c, n, gate, dtype, ws, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(u=None), EINVAL), (dict(w=None), EINVAL), (dict(y=None), EINVAL), (dict(b=-1), EINVAL), (dict(c=0), EINVAL), (dict(n=0), EINVAL), (dict(n=1 << 31), EINVAL),
+    (dict(b=1 << 20, c=1 << 12), EINVAL), (dict(gate=2), EINVAL), (dict(gate=-1), EINVAL), (dict(dtype=3), EINVAL), (dict(u=A + 1), EINVAL), (dict(v=A + 1), EINVAL),
+    (dict(w=A + 2, dtype=F32), EINVAL), (dict(state=A + 2), EINVAL), (dict(lengths=A + 2), EINVAL), (dict(last=A + 1), EINVAL), (dict(kept=A + 2), EINVAL),
+    (dict(ws=None, n=100000), EINVAL), (dict(ws=A + 4), EINVAL), (dict(b=0, u=None, w=None, y=None), OK),
+])
+def test_scan(kw, rc):
+    assert scan(**kw) == rc
+
+
+def back(dy=A, u=A, w=A, v=A, kept=A, dlast=A, lengths=A, du=A, dw=A, dv=A, dstate=A, b=2, c=3, n=100, gate=1, dtype=F16, ws=A):
+    return call("fftconv_gated_scan_backward", dy, u, w, v, kept, dlast, lengths, du, dw, dv, dstate, b, c, n, gate, dtype, ws, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(dy=None), EINVAL), (dict(u=None), EINVAL), (dict(w=None), EINVAL), (dict(kept=None), EINVAL), (dict(du=None), EINVAL), (dict(dw=None), EINVAL),
+    (dict(v=None), EINVAL), (dict(dv=None), EINVAL), (dict(gate=7), EINVAL), (dict(dtype=-1), EINVAL), (dict(dy=A + 1), EINVAL), (dict(kept=A + 2), EINVAL),
+    (dict(dlast=A + 1), EINVAL), (dict(dstate=A + 2), EINVAL), (dict(du=A + 1), EINVAL), (dict(ws=None, n=5000), EINVAL), (dict(n=0), EINVAL), (dict(c=-1), EINVAL),
+    (dict(b=0, dy=None, u=None, w=None, kept=None, du=None, dw=None), OK),
+])
+def test_scan_backward(kw, rc):
+    assert back(**kw) == rc
+
+
+def test_step():
+    def step(u=A, w=A, v=None, state=A, to=A, y=A, t=5, gate=0, dtype=F32):
+        return call("fftconv_gated_step", u, w, v, state, to, y, t, gate, dtype, None)
+    for kw in (dict(u=None), dict(w=None), dict(state=None), dict(to=None), dict(y=None), dict(t=-1), dict(t=1 << 31), dict(gate=3), dict(dtype=5), dict(u=A + 2),
+               dict(state=A + 1), dict(to=A + 2), dict(v=A + 2)):
+        assert step(**kw) == EINVAL, kw
+    assert step(t=0, u=None, w=None, state=None, to=None, y=None) == OK
+
+
+def linear(x=A, xs=A, w=A, ws=A, bias=None, y=A, b=2, n=3, k=64, o=12, parts=0, dtype=BF16, work=A):
+    return call("fftconv_linear_f8", x, xs, w, ws, bias, y, b, n, k, o, parts, dtype, work, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(x=None), EINVAL), (dict(xs=None), EINVAL), (dict(w=None), EINVAL), (dict(ws=None), EINVAL), (dict(y=None), EINVAL), (dict(b=-1), EINVAL), (dict(n=0), EINVAL),
+    (dict(k=0), EINVAL), (dict(o=0), EINVAL), (dict(o=(1 << 31) - 511), EINVAL), (dict(b=1 << 16, n=1 << 16), EINVAL), (dict(parts=-1), EINVAL), (dict(parts=5), EINVAL),
+    (dict(dtype=4), EINVAL), (dict(xs=A + 2), EINVAL), (dict(ws=A + 1), EINVAL), (dict(bias=A + 2), EINVAL), (dict(y=A + 1), EINVAL),
+    (dict(b=1, n=100, k=4096, o=512, work=None), EINVAL), (dict(work=A + 2), EINVAL), (dict(k=(1 << 20) + 1), EUNSUPPORTED),
+    (dict(b=1 << 15, n=1 << 15, o=1 << 20), EUNSUPPORTED), (dict(b=0, x=None, xs=None, w=None, ws=None, y=None), OK),
+])
+def test_linear(kw, rc):
+    assert linear(**kw) == rc
+
+
+def test_quantisers():
+    def rows(x=A, ld=64, q=A, s=A, t=2, k=64, dtype=F16):
+        return call("fftconv_quantize_blocks", x, ld, q, s, t, k, dtype, None)
+    for kw in (dict(x=None), dict(q=None), dict(s=None), dict(ld=63), dict(ld=1 << 40), dict(dtype=9), dict(s=A + 1), dict(x=A + 1), dict(k=0), dict(t=-1), dict(t=1 << 31)):
+        assert rows(**kw) == EINVAL, kw
+    assert rows(k=1 << 21, ld=1 << 21) == EUNSUPPORTED and rows(t=0, x=None) == OK
+
+    def channels(x=A, q=A, s=A, b=2, n=5, k=12, parts=3, dtype=F32):
+        return call("fftconv_quantize_blocks_channels", x, q, s, b, n, k, parts, dtype, None)
+    for kw in (dict(x=None), dict(q=None), dict(s=None), dict(b=-1), dict(n=0), dict(k=0), dict(parts=0), dict(parts=5), dict(dtype=7), dict(x=A + 2), dict(s=A + 2),
+               dict(b=1 << 20, n=1 << 20)):
+        assert channels(**kw) == EINVAL, kw
+    assert channels(k=3 << 20) == EUNSUPPORTED and channels(b=0, x=None) == OK
+
+    def tiles(x=A, ld=64, q=A, s=A, qt=A, st=A, o=5, k=64, dtype=F32):
+        return call("fftconv_quantize_tiles", x, ld, q, s, qt, st, o, k, dtype, None)
+    for kw in (dict(x=None), dict(q=None), dict(s=None), dict(qt=None), dict(st=None), dict(q=None, s=None, qt=None, st=None), dict(ld=3), dict(o=0), dict(k=0),
+               dict(dtype=-1), dict(x=A + 2), dict(s=A + 2), dict(st=A + 1), dict(o=1 << 31)):
+        assert tiles(**kw) == EINVAL, kw
+
+
+def clip(at=(A,), out=(A,), counts=(10,), types=(F32,), types_out=None, n=None, limit=1.0, eps=1e-6, given=None, norm=A, ws=A, arrays=True):
+    i64, ints = (lambda v: None if v is None else (ctypes.c_int64 * max(1, len(v)))(*v)), (lambda v: None if v is None else (ctypes.c_int * max(1, len(v)))(*v))
+    a = [i64(at), i64(out), i64(counts), ints(types), ints(types_out)]
+    return call("fftconv_clip_grads", *a, len(at) if n is None else n, limit, eps, given, norm, ws, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n=-1), dict(counts=(-1,)), dict(counts=((1 << 40) + 1,)), dict(at=(None or 0,)), dict(out=(0,)), dict(types=(3,)), dict(types=(F32,), types_out=(BF16,)),
+    dict(types=(BF16,), types_out=(F16,)), dict(at=(A + 2,)), dict(out=(A + 2,)), dict(limit=-1.0), dict(limit=float("nan")), dict(eps=-1.0), dict(eps=float("nan")),
+    dict(limit=0.0, eps=0.0), dict(ws=None), dict(ws=A + 4), dict(norm=A + 2), dict(given=A + 1), dict(out=None, given=A), dict(counts=None), dict(types=None),
+    # what is written twice, or while it is read
+    dict(at=(A, A), out=(A, A), counts=(10, 10), types=(F32, F32)), dict(at=(A, 9 * A), out=(A, A + 36), counts=(10, 10), types=(F32, F32)),
+    dict(at=(A, 9 * A), out=(9 * A, A), counts=(10, 10), types=(F32, F32)), dict(at=(A,), out=(A + 4,)), dict(at=(A,), out=(A - 4,)),
+    dict(at=(A,), out=(A,), types=(BF16,), types_out=(F32,)), dict(at=(A,), out=(A - 20,), types=(BF16,), types_out=(F32,)),
+    dict(at=(A, A + 8, 5 * A), out=(6 * A, 7 * A, A + 40), counts=(10, 20, 2), types=(F32,) * 3),
+    dict(at=tuple(A * (i + 1) for i in range(300)), out=tuple(A * (i + 1) for i in range(299)) + (A * 7 + 4,), counts=(3,) * 300, types=(F32,) * 300),
+])
+def test_clip(kw):
+    assert clip(**kw) == EINVAL
+
+
+def test_workspaces():
+    lib = fftconv.load()
+    assert lib.fftconv_workspace_bytes_gated_scan(1, 16, 131072, F32) > 0 and lib.fftconv_workspace_bytes_gated_scan(64, 768, 4096, BF16) == 0
+    assert lib.fftconv_workspace_bytes_gated_scan(1, 16, 0, F32) == 0 and lib.fftconv_workspace_bytes_gated_scan(1, 16, 131072, 9) == 0
+    assert lib.fftconv_workspace_bytes_linear_f8(1, 100, 4096, 512, 0, F32) > 0 and lib.fftconv_workspace_bytes_linear_f8(1, 1, 4096, 512, 0, F32) == 0
+    counts = (ctypes.c_int64 * 3)(5, 0, 1 << 40)
+    assert lib.fftconv_workspace_bytes_clip_grads(counts, 3) >= 16 and lib.fftconv_workspace_bytes_clip_grads(None, 0) >= 8
+    counts[0] = -1
+    assert lib.fftconv_workspace_bytes_clip_grads(counts, 3) == 0 and lib.fftconv_workspace_bytes_clip_grads(None, 2) == 0
