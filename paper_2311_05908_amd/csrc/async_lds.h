@@ -31,6 +31,10 @@ __device__ __forceinline__ void to_lds4(const char *base, uint32_t off, const ch
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(off), "s"(base) : "memory");
 }
+__device__ __forceinline__ void to_lds4(const char *from, const char *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds_offset(to))), "v"(from) : "memory");
+}
 // N such in a row, 1024 bytes apart in LDS. The instruction's own offset moves both addresses, so off[i] is 1024 i less than the distance from base
 // (callers keep base below the first byte by as much as that needs).
 template <int N> __device__ __forceinline__ void to_lds16_rows(const char *base, const uint32_t (&off)[N], uint32_t to)

@@ -33,6 +33,10 @@ __device__ __forceinline__ uint4 load16(const void *bytes, int64_t k, int64_t K)
     return v;
 }
 
+// The place in LDS of 16-byte piece c (0 .. 3) of a 64-byte row. A clock delivers 256 bytes, here the same piece of sixteen rows in a run: four rows
+// lie in 256 bytes, so the piece is moved by the row's number above that, and all sixteen come from banks of their own.
+__device__ __forceinline__ int piece_at(int row, int c) { return row * 64 + ((c ^ ((row >> 2) & 3)) << 4); }
+
 // 16 bytes to y. Past the caches where y would only push everything else out of the memory-side one: bf16 64 x 4096 x 768 -> 3 x 768, 1.2 GB, 643 -> 619 us;
 // f16 8192 x 4096 -> 16384, 0.27 GB, 505 us with and 512 without them.
 template <bool BEYOND> __device__ __forceinline__ void put16(char *to, uint4 v)

@@ -69,19 +69,21 @@ __device__ __forceinline__ bf16x8 widened(uint32_t lo, uint32_t hi)
 // instruction for any of the 8-bit formats; measured with one product of 2^16 and one of 2^16 down to 2^-9 beside it). On normally distributed values that is
 // 1.3e-5 of the result: for results in 16 bits, whose own rounding is 2e-4 and more, of no account; fp32 results take the values to bf16, which
 // holds them, and bf16's products, which are exact, at half the rate.
+template <bool CLOSE> __device__ __forceinline__ void product_of(const Half &r, const Half &s, f32x16 &c)
+{
+    if constexpr (!CLOSE) {
+        c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(r), operand(s), c, 0, 0, 0, 0, 0, 0);
+    } else {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r.a.x, r.a.y), widened(s.a.x, s.a.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r.a.z, r.a.w), widened(s.a.z, s.a.w), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r.b.x, r.b.y), widened(s.b.x, s.b.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r.b.z, r.b.w), widened(s.b.z, s.b.w), c, 0, 0, 0);
+    }
+}
 template <bool CLOSE> __device__ __forceinline__ void products(const Half (&r)[2], const Half (&s)[2], f32x16 &c)
 {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-        if constexpr (!CLOSE) {
-            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(r[kk]), operand(s[kk]), c, 0, 0, 0, 0, 0, 0);
-        } else {
-            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r[kk].a.x, r[kk].a.y), widened(s[kk].a.x, s[kk].a.y), c, 0, 0, 0);
-            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r[kk].a.z, r[kk].a.w), widened(s[kk].a.z, s[kk].a.w), c, 0, 0, 0);
-            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r[kk].b.x, r[kk].b.y), widened(s[kk].b.x, s[kk].b.y), c, 0, 0, 0);
-            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened(r[kk].b.z, r[kk].b.w), widened(s[kk].b.z, s[kk].b.w), c, 0, 0, 0);
-        }
-    }
+    product_of<CLOSE>(r[0], s[0], c);
+    product_of<CLOSE>(r[1], s[1], c);
 }
 template <bool CLOSE> __device__ __forceinline__ f32x4 products16(const Half &r, const Half &s)
 {
@@ -200,88 +202,68 @@ template <typename T, int FR, int FS> __global__ void __launch_bounds__(256, 2) 
 // a row of eight rows, whole lines, instead of scattered words. An accumulator's values go there with the bias, rounded, in rows of y; 16-byte pieces
 // (in rows of 64 bytes: rows) are moved so that the lanes that write at once meet no bank twice.
 //
-// Token by token: a row of 128 bytes to a token, 64 outputs (32 of fp32), of which this is part `part`. The halves of a piece change places in tokens 16 up.
-template <typename T> __device__ __forceinline__ void tokens_to_lds(char *own, const f32x16 &acc, int part, const float *bias)
+// Token by token: rows of ROW bytes to a token. 128: 64 outputs, of which this is part `part`; the halves of a piece change places in tokens 16 up. 64: 32 outputs.
+template <typename T, int ROW> __device__ __forceinline__ void tokens_to_lds(char *own, const f32x16 &acc, int part, const float *bias)
 {
     const int half = (threadIdx.x >> 5) & 1, l32 = threadIdx.x & 31;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const f32x4 b = *(const f32x4 *)(bias + 8 * q + 4 * half);
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = acc[4 * q + i] + b[i];
-        if constexpr (sizeof(T) == 4) {
-            *(float4 *)(own + l32 * 128 + (((2 * q + half) ^ ((l32 >> 1) & 7)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
-            const T t[4] = {from_f32<T>(v[0]), from_f32<T>(v[1]), from_f32<T>(v[2]), from_f32<T>(v[3])};
-            uint2 w;
-            __builtin_memcpy(&w, t, 8);
-            *(uint2 *)(own + l32 * 128 + (((4 * part + q) ^ ((l32 >> 1) & 7)) << 4) + ((half ^ (l32 >> 4)) << 3)) = w;
-        }
+        const T t[4] = {from_f32<T>(acc[4 * q] + b[0]), from_f32<T>(acc[4 * q + 1] + b[1]), from_f32<T>(acc[4 * q + 2] + b[2]), from_f32<T>(acc[4 * q + 3] + b[3])};
+        uint2 w;
+        __builtin_memcpy(&w, t, 8);
+        const int at = ROW == 128 ? (((4 * part + q) ^ ((l32 >> 1) & 7)) << 4) + ((half ^ (l32 >> 4)) << 3) : ((q ^ ((l32 >> 2) & 3)) << 4) + (half << 3);
+        *(uint2 *)(own + l32 * ROW + at) = w;
     }
 }
-// Piece lane % 8 of row lane / 8 + 8 t of what lies there.
-template <typename T> __device__ __forceinline__ uint4 token_piece(const char *own, int t)
+// Pieces t of a lane: of row lane / 8 + 8 t piece lane % 8 (128-byte rows), of row lane / 4 + 16 t piece lane % 4 (64-byte ones).
+template <int ROW> __device__ __forceinline__ uint4 token_piece(const char *own, int t)
 {
-    const int lane = threadIdx.x & 63, c = (lane >> 3) + 8 * t;
-    const uint4 v = *(const uint4 *)(own + c * 128 + (((lane & 7) ^ ((c >> 1) & 7)) << 4));
-    return sizeof(T) == 2 && t >= 2 ? make_uint4(v.z, v.w, v.x, v.y) : v;
+    const int lane = threadIdx.x & 63;
+    if constexpr (ROW == 64) {
+        const int c = (lane >> 2) + 16 * t;
+        return *(const uint4 *)(own + c * 64 + (((lane & 3) ^ ((c >> 2) & 3)) << 4));
+    } else {
+        const int c = (lane >> 3) + 8 * t;
+        const uint4 v = *(const uint4 *)(own + c * 128 + (((lane & 7) ^ ((c >> 1) & 7)) << 4));
+        return t >= 2 ? make_uint4(v.z, v.w, v.x, v.y) : v;
+    }
 }
-// Channel by channel: rows of WIDE tokens to an output. 64 tokens of 16 bits or 32 of fp32: 32 rows of 128 bytes, `part` says which 32 of the tokens; 32 of 16 bits:
-// 64 rows of 64 bytes, `part` says which 32 of the rows. 16-bit values of two neighbouring lanes change places so that each lane writes a word: the even
-// one of the first of two outputs, the odd one of the second.
+// Channel by channel: rows of WIDE tokens to an output: 64, of which this is 32-token part `part`, or 32. Values of two neighbouring lanes change places so
+// that each lane writes a word: the even one of the first of two outputs, the odd one of the second.
 template <typename T, int WIDE> __device__ __forceinline__ void channels_to_lds(char *own, const f32x16 &acc, int part, const float *bias)
 {
     const int half = (threadIdx.x >> 5) & 1, l32 = threadIdx.x & 31, odd = l32 & 1;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const f32x4 b = *(const f32x4 *)(bias + 8 * q + 4 * half);
-        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 8 * q + 4 * half + i;
-                *(float *)(own + row * 128 + (((l32 >> 2) ^ ((row >> 2) & 1)) << 4) + (l32 & 3) * 4) = acc[4 * q + i] + b[i];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                const T t[2] = {from_f32<T>(acc[4 * q + i] + b[i]), from_f32<T>(acc[4 * q + i + 1] + b[i + 1])};
-                uint32_t w;
-                __builtin_memcpy(&w, t, 4);
-                const uint32_t n = dpp<0xB1>(w);                 // the neighbour's
-                const uint32_t o = __builtin_amdgcn_perm(n, w, odd ? 0x03020706u : 0x05040100u);
-                const int row = 8 * q + 4 * half + i + odd, moved = (row >> 2) & 1;
-                if constexpr (WIDE == 64) {
-                    const int piece = part * 4 + (l32 >> 3);
-                    *(uint32_t *)(own + row * 128 + ((piece ^ (moved << 2)) << 4) + ((l32 >> 1) & 3) * 4) = o;
-                } else {
-                    *(uint32_t *)(own + (part * 32 + (row ^ (moved << 1))) * 64 + (l32 >> 1) * 4) = o;
-                }
-            }
+        for (int i = 0; i < 4; i += 2) {
+            const T t[2] = {from_f32<T>(acc[4 * q + i] + b[i]), from_f32<T>(acc[4 * q + i + 1] + b[i + 1])};
+            uint32_t w;
+            __builtin_memcpy(&w, t, 4);
+            const uint32_t n = dpp<0xB1>(w);                     // the neighbour's
+            const uint32_t o = __builtin_amdgcn_perm(n, w, odd ? 0x03020706u : 0x05040100u);
+            const int row = 8 * q + 4 * half + i + odd, moved = (row >> 2) & 1;
+            if constexpr (WIDE == 64) *(uint32_t *)(own + row * 128 + (((part * 4 + (l32 >> 3)) ^ (moved << 2)) << 4) + ((l32 >> 1) & 3) * 4) = o;
+            else *(uint32_t *)(own + (row ^ (moved << 1)) * 64 + (l32 >> 1) * 4) = o;
         }
     }
 }
-// Pieces t = 0 ... 3 of a lane: of row lane / 8 + 8 t piece lane % 8, or of 64-byte rows, of row lane / 4 + 16 t piece lane % 4.
-template <typename T, int WIDE> __device__ __forceinline__ uint4 output_piece(const char *own, int t)
+template <int WIDE> __device__ __forceinline__ uint4 output_piece(const char *own, int t)
 {
-    const int lane = threadIdx.x & 63;
-    if constexpr (sizeof(T) == 2 && WIDE == 32) {
-        const int row = (lane >> 2) + 16 * t;
-        return *(const uint4 *)(own + (row ^ (((row >> 2) & 1) << 1)) * 64 + ((lane & 3) << 4));
-    } else {
-        const int row = (lane >> 3) + 8 * t, moved = (row >> 2) & 1;
-        return *(const uint4 *)(own + row * 128 + (((lane & 7) ^ (sizeof(T) == 2 ? moved << 2 : moved)) << 4));
-    }
+    const int lane = threadIdx.x & 63, row = WIDE == 32 ? (lane >> 2) + 16 * t : (lane >> 3) + 8 * t, moved = (row >> 2) & 1;
+    if constexpr (WIDE == 32) return *(const uint4 *)(own + (row ^ (moved << 1)) * 64 + ((lane & 3) << 4));
+    else return *(const uint4 *)(own + row * 128 + (((lane & 7) ^ (moved << 2)) << 4));
 }
 
 // The same for operands in pieces of 16 bytes (K a multiple of 16): 2 x 4 waves, pieces straight to LDS, a block of 128 while the one before it is
 // multiplied, in one stream over a workgroup's tiles. A wave holds the tokens' operands of a block and brings the weight's 32 rows at a time, one group
 // ahead; sums of a block are two accumulators in turn, added to the totals while the next products run.
-template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void __launch_bounds__(512, 2) k_f8_async(const F8Args a, const Walk walk)
+template <typename T, bool CHANNELS> __global__ void __launch_bounds__(512, 2) k_f8_large(const F8Args a, const Walk walk)
 {
-    constexpr int BR = 64 * FR, BS = 128 * FS, STAGE = (BR + BS) * 128, LI = (BR + BS) / 64;
-    constexpr bool CLOSE = sizeof(T) == 4;
-    static_assert(BR == BS && LI % 4 == 0, "waves 0-3 bring the weight, 4-7 bring the tokens");
+    constexpr int FR = 4, FS = 2, BR = 64 * FR, BS = 128 * FS, STAGE = (BR + BS) * 128, LI = (BR + BS) / 64;
+    static_assert(BR == BS && LI % 4 == 0 && sizeof(T) == 2, "waves 0-3 bring the weight, 4-7 bring the tokens");
     extern __shared__ __align__(16) char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
     const int wr = wave >> 2, wsv = wave & 3;
@@ -290,12 +272,6 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
     const int begin = (int)((int64_t)walk.tiles * die / dies), last = (int)((int64_t)walk.tiles * (die + 1) / dies);
     const int first = begin + blockIdx.x / 8;
     const bool tail = a.K % 128 != 0;
-    // item i of the walk: tile i / ranges, range i % ranges of k
-    auto item = [&](int i, int &tr, int &ts, int &range) {
-        range = SPLIT ? i % a.ranges : 0;
-        walk.place(SPLIT ? i / a.ranges : i, tr, ts, a.tiles_r);
-    };
-    auto blocks_of = [&](int range) { return SPLIT ? min(a.per, a.blocks - range * a.per) : a.blocks; };
 
     // This wave brings rows LI * 8 * (wave % 4) ... of the weight (waves 0-3) or the tokens (4-7), eight with an instruction, a piece of 16 bytes for each
     // lane, moved as piece128 has it; and, for itself, the scales of its 32 FS tokens and of its outputs.
@@ -304,32 +280,31 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * LI * 1024;
     constexpr int OWN = 512, PRIVATE = 2 * OWN + FR * 128;       // a stage's scales of a wave; both stages' and the bias of its outputs
     char *const own = lds + 2 * STAGE + wave * PRIVATE;
-    int f_tile = first, f_step = 0, f_steps = 0, f_first = 0;    // what is asked for next; blocks of its range, and of those before it
+    int f_tile = first, f_step = 0;                              // what is asked for next
     const char *base = nullptr, *xs = nullptr, *ws = nullptr;
     uint32_t off[LI], xs_off = 0;
     auto aim = [&] {                                             // at tile f_tile, or, after the last, once more at it
-        int tr, ts, range;
-        item(min(f_tile, last - 1), tr, ts, range);
-        f_steps = blocks_of(range), f_first = SPLIT ? range * a.per : 0;
+        int tr, ts;
+        walk.place(min(f_tile, last - 1), tr, ts, a.tiles_r);
         const int row0 = (is_r ? tr : ts) * block;
-        base = (const char *)(is_r ? a.w : a.x) + (int64_t)row0 * a.K + (int64_t)f_first * 128 - 3072;
+        base = (const char *)(is_r ? a.w : a.x) + (int64_t)row0 * a.K - 3072;
 #pragma unroll
         for (int i = 0; i < LI; ++i) {
             const int row = (wave & 3) * 8 * LI + i * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
             off[i] = (uint32_t)(min(row0 + row, rows - 1) - row0) * (uint32_t)a.K + piece * 16 + 3072 - (i % 4) * 1024;
         }
         const int s0 = ts * BS;
-        xs = (const char *)(a.xs + (int64_t)f_first * a.T + s0);
+        xs = (const char *)(a.xs + s0);
         xs_off = (uint32_t)(min(s0 + wsv * FS * 32 + (FS == 2 ? lane : l32), a.T - 1) - s0) * 4u;
-        ws = (const char *)(a.ws + (int64_t)min((tr * BR + wr * FR * 32) / 128, a.row_tiles - 1) * a.blocks + f_first);
+        ws = (const char *)(a.ws + (int64_t)min((tr * BR + wr * FR * 32) / 128, a.row_tiles - 1) * a.blocks);
     };
     auto fetch = [&](int stage) {
-        if (tail && f_first + f_step == a.blocks - 1) {          // what lies beyond K reads as zeros
+        if (tail && f_step == a.blocks - 1) {          // what lies beyond K reads as zeros
 #pragma unroll
             for (int i = 0; i < LI; ++i) {
                 const int row = (wave & 3) * 8 * LI + i * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
                 const char *const from = base + off[i] + (i % 4) * 1024;
-                to_lds16((int64_t)(f_first + f_step) * 128 + piece * 16 < a.K ? from : (const char *)&zero_piece, lds + stage * STAGE + (wave * LI + i) * 1024);
+                to_lds16((int64_t)f_step * 128 + piece * 16 < a.K ? from : (const char *)&zero_piece, lds + stage * STAGE + (wave * LI + i) * 1024);
             }
         } else {
 #pragma unroll
@@ -341,7 +316,7 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
         to_lds4(uniform(xs), xs_off, own + stage * OWN);
         to_lds4(uniform(ws), 0, own + stage * OWN + 256);
         base += 128, xs += (int64_t)a.T * 4, ws += 4;
-        if (++f_step == f_steps) {
+        if (++f_step == a.blocks) {
             f_step = 0, f_tile += on_die;
             aim();
         }
@@ -364,16 +339,13 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
 #pragma unroll
     for (int j = 0; j < FS; ++j) read(fs[j], lds + j * 4096, so);
     for (int tile = first; tile < last; tile += on_die) {
-        int tr, ts, range;
-        item(tile, tr, ts, range);
-        const int steps = blocks_of(range);
-        if (!SPLIT) {
-            const int r0 = tr * BR;
-            const char *const bias = uniform(a.bias ? (const char *)(a.bias + r0) : (const char *)&zero_piece);
+        int tr, ts;
+        walk.place(tile, tr, ts, a.tiles_r);
+        const int steps = a.blocks;
+        const char *const bias = uniform(a.bias ? (const char *)(a.bias + tr * BR) : (const char *)&zero_piece);
 #pragma unroll
-            for (int i = 0; i < FR; i += 2)
-                to_lds4(bias, a.bias ? (uint32_t)(min(r0 + (wr * FR + i) * 32 + lane, a.O - 1) - r0) * 4u : 0u, own + 2 * OWN + i * 128);
-        }
+        for (int i = 0; i < FR; i += 2)
+            to_lds4(bias, a.bias ? (uint32_t)(min(tr * BR + (wr * FR + i) * 32 + lane, a.O - 1) - tr * BR) * 4u : 0u, own + 2 * OWN + i * 128);
         f32x16 acc[FR][FS] = {};
         for (int k = 0; k < steps; ++k) {
             const char *const here = lds + stage * STAGE, *const scales = own + stage * OWN;
@@ -396,7 +368,7 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
 #pragma unroll
                 for (int j = 0; j < FS; ++j) {
                     p[j] = f32x16{};
-                    products<CLOSE>(fr[i & 1], fs[j], p[j]);
+                    products<false>(fr[i & 1], fs[j], p[j]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (i + 1 == FR) {
@@ -416,23 +388,6 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
         asm volatile("" : "+v"(lane));                           // (else the compiler keeps the places below in registers throughout the sums)
         const int l32 = lane & 31, half = lane >> 5, r0 = tr * BR, s0 = ts * BS;
         const int r1 = r0 + wr * FR * 32, s1 = s0 + wsv * FS * 32;
-        if constexpr (SPLIT) {
-            float *const part = a.part + (int64_t)range * a.T * a.O;
-#pragma unroll
-            for (int i = 0; i < FR; ++i)
-#pragma unroll
-                for (int j = 0; j < FS; ++j) {
-                    const int t = s1 + j * 32 + l32, o = r1 + i * 32 + 4 * half;
-                    if (t >= a.T) continue;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                        if (o + 8 * q < a.O) store_piece<float, 4>(part + (int64_t)t * a.O + o + 8 * q, a.O - o - 8 * q, v);
-                    }
-                }
-            fetch(stage ^ 1);
-            continue;
-        }
         // All of it inside y, in one sequence and one part of y: places are linear in rows and columns.
         bool whole = r0 + BR <= a.O && s0 + BS <= a.T && (CHANNELS ? a.N : a.O) < 1 << 26;        // (32-bit distances of seven rows)
         if (CHANNELS)
@@ -443,23 +398,22 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
             static_assert(LI >= 4, "a wave's results fit where its transfers go");
             char *const mine = lds + (stage ^ 1) * STAGE + wave * LI * 1024;
             const float *const bias = (const float *)(own + 2 * OWN);
-            constexpr int W = 16 / sizeof(T), WIDE = FS == 2 ? 64 : 32;
-            constexpr bool NARROW = CHANNELS && sizeof(T) == 2 && FS == 1;     // rows of 64 bytes
+            constexpr int W = 8;
             const uint32_t stride = CHANNELS ? (uint32_t)a.N : (uint32_t)a.O;
             const char *const y = uniform((const char *)((T *)a.y + token_of(a, s1) + output_of(a, r1)));
-            const uint32_t at = ((uint32_t)(lane >> (NARROW ? 2 : 3)) * stride + (lane & (NARROW ? 3 : 7)) * W) * (uint32_t)sizeof(T);
+            const uint32_t at = ((uint32_t)(lane >> 3) * stride + (lane & 7) * W) * 2u;
             auto all = [&](auto beyond) {
                 // four pieces a lane, from row i (of 32 outputs) and column j (of 32 tokens) on
                 auto out = [&](int i, int j) {
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const uint4 v = CHANNELS ? output_piece<T, WIDE>(mine, t) : token_piece<T>(mine, t);
-                        const int row = (NARROW ? 16 : 8) * t;
+                        const uint4 v = CHANNELS ? output_piece<64>(mine, t) : token_piece<128>(mine, t);
+                        const int row = 8 * t;
                         const int64_t place = CHANNELS ? (int64_t)(i * 32 + row) * stride + j * 32 : (int64_t)(j * 32 + row) * stride + i * 32;
-                        put16<decltype(beyond)::value>((char *)y + place * (int)sizeof(T) + at, v);
+                        put16<decltype(beyond)::value>((char *)y + place * 2 + at, v);
                     }
                 };
-                constexpr int PI = sizeof(T) == 2 && (!CHANNELS || FS == 1) ? 2 : 1, PJ = sizeof(T) == 2 && CHANNELS && FS == 2 ? 2 : 1;
+                constexpr int PI = CHANNELS ? 1 : 2, PJ = CHANNELS ? 2 : 1;
 #pragma unroll
                 for (int i = 0; i < FR; i += PI)
 #pragma unroll
@@ -469,8 +423,8 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
                         for (int p = 0; p < PI; ++p)
 #pragma unroll
                             for (int q = 0; q < PJ; ++q) {
-                                if constexpr (CHANNELS) channels_to_lds<T, WIDE>(mine, acc[i + p][j + q], p + q, bias + (i + p) * 32);
-                                else tokens_to_lds<T>(mine, acc[i + p][j + q], p, bias + (i + p) * 32);
+                                if constexpr (CHANNELS) channels_to_lds<T, 64>(mine, acc[i + p][j + q], q, bias + (i + p) * 32);
+                                else tokens_to_lds<T, 128>(mine, acc[i + p][j + q], p, bias + (i + p) * 32);
                             }
                         out(i, j);
                     }
@@ -491,6 +445,186 @@ template <typename T, bool CHANNELS, bool SPLIT, int FR, int FS> __global__ void
         }
         __builtin_amdgcn_sched_barrier(0);
         fetch(stage ^ 1);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // nothing is on its way to LDS when the workgroup ends
+}
+
+// Tiles of 128 x 128, where there are too few of 256 x 256: 2 x 4 waves of 64 outputs by 32 tokens, four steps of 64 of k in LDS, asked for three steps ahead,
+// for here it is how long a transfer takes that counts (4096 x 768 -> 2304: six blocks to a tile). Sums of a block stay in their accumulators over its two
+// steps. Two workgroups share a compute unit.
+template <typename T, bool CHANNELS, bool SPLIT> __global__ void __launch_bounds__(512, 4) k_f8_small(const F8Args a, const Walk walk)
+{
+    constexpr int FR = 2, BR = 128, BS = 128, BK = 64, STAGE = (BR + BS) * BK, STAGES = 4;
+    constexpr bool CLOSE = sizeof(T) == 4;
+    extern __shared__ __align__(16) char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+    const int wr = wave >> 2, wsv = wave & 3;
+    // tiles first, first + stride, ... below last
+    const int wgs = gridDim.x, die = blockIdx.x % 8, dies = min(8, wgs), on_die = (wgs - die + 7) / 8;
+    const int begin = (int)((int64_t)walk.tiles * die / dies), last = (int)((int64_t)walk.tiles * (die + 1) / dies);
+    const int first = begin + blockIdx.x / 8;
+    const int all_steps = (int)((a.K + BK - 1) / BK);
+    const bool tail = a.K % BK != 0;
+    // item i of the walk: tile i / ranges, range i % ranges of k
+    auto item = [&](int i, int &tr, int &ts, int &range) {
+        range = SPLIT ? i % a.ranges : 0;
+        walk.place(SPLIT ? i / a.ranges : i, tr, ts, a.tiles_r);
+    };
+    auto steps_of = [&](int range) { return SPLIT ? min(2 * a.per, all_steps - 2 * range * a.per) : all_steps; };
+
+    // This wave brings 32 rows of the weight (waves 0-3) or the tokens (4-7), sixteen with an instruction, a piece of 16 bytes for each lane, moved as
+    // piece_at has it; and, for itself, with a block's first step, the scales of its 32 tokens (lanes 0-31) and of its outputs (one, in lanes 32-63).
+    const bool is_r = wave < 4;
+    const int rows = is_r ? a.O : a.T;
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * 2048;
+    char *const own = lds + STAGES * STAGE + wave * (STAGES * 256 + 256);
+    int f_tile = first, f_step = 0, f_steps = 0, f_first = 0;    // what is asked for next; steps of its range, and of those before it
+    const char *base = nullptr, *scale = nullptr;
+    uint32_t off[2];
+    auto aim = [&] {                                             // at tile f_tile, or, after the last, once more at it
+        int tr, ts, range;
+        item(min(f_tile, last - 1), tr, ts, range);
+        f_steps = steps_of(range), f_first = SPLIT ? 2 * range * a.per : 0;
+        const int row0 = (is_r ? tr : ts) * 128;
+        base = (const char *)(is_r ? a.w : a.x) + (int64_t)row0 * a.K + (int64_t)f_first * BK - 1024;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = (wave & 3) * 32 + i * 16 + (lane >> 2), piece = (lane & 3) ^ ((row >> 2) & 3);
+            off[i] = (uint32_t)(min(row0 + row, rows - 1) - row0) * (uint32_t)a.K + piece * 16 + 1024 - i * 1024;
+        }
+        scale = half == 0 ? (const char *)(a.xs + (int64_t)(f_first / 2) * a.T + min(ts * BS + wsv * 32 + l32, a.T - 1))
+                          : (const char *)(a.ws + (int64_t)min(tr, a.row_tiles - 1) * a.blocks + f_first / 2);
+    };
+    const int64_t scale_step = half == 0 ? (int64_t)a.T * 4 : 4;
+    auto fetch = [&](int stage) {
+        if (tail && f_first + f_step == all_steps - 1) {         // what lies beyond K reads as zeros
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int piece = (lane & 3) ^ ((lane >> 4) & 3);
+                const char *const from = base + off[i] + i * 1024;
+                to_lds16((int64_t)(f_first + f_step) * BK + piece * 16 < a.K ? from : (const char *)&zero_piece, lds + stage * STAGE + wave * 2048 + i * 1024);
+            }
+        } else {
+            to_lds16_rows<2>(uniform(base), off, __builtin_amdgcn_readfirstlane(to + stage * STAGE));
+        }
+        if (f_step % 2 == 0) {
+            to_lds4(scale, own + stage * 256);
+            scale += scale_step;
+        }
+        base += BK;
+        if (++f_step == f_steps) {
+            f_step = 0, f_tile += on_die;
+            aim();
+        }
+    };
+
+    if (first >= last) return;
+    aim();
+    fetch(0);
+    fetch(1);
+    fetch(2);
+    // where this lane's pieces are, from a stage's start: half of a row's, and the other two at ^ 32
+    const int ro = piece_at(wr * FR * 32 + l32, half), so = BR * BK + piece_at(wsv * 32 + l32, half);
+    int stage = 0;
+    for (int tile = first; tile < last; tile += on_die) {
+        int tr, ts, range;
+        item(tile, tr, ts, range);
+        const int steps = steps_of(range), r0 = tr * BR, s0 = ts * BS;
+        if (!SPLIT)
+            to_lds4(uniform(a.bias ? (const char *)(a.bias + r0) : (const char *)&zero_piece), a.bias ? (uint32_t)(min(r0 + wr * FR * 32 + lane, a.O - 1) - r0) * 4u : 0u,
+                    own + STAGES * 256);
+        f32x16 acc[FR] = {}, p[FR];
+        float s = 0.f;
+        auto step = [&](auto which, int k) {
+            constexpr int KK = decltype(which)::value;
+            FC_ARRIVED(2 + 3);                                   // this step's pieces are there (of the two after it, three and two transfers); every wave has read the last one's
+            const char *const here = lds + stage * STAGE, *const scales = own + stage * 256;
+            const int free_stage = stage == 0 ? STAGES - 1 : stage - 1;
+            // (the tile's last one is asked for after its results, which go by way of that stage)
+            if (k + 1 < steps) fetch(free_stage);
+            if (KK == 0) s = *(const float *)(scales + l32 * 4) * *(const float *)(scales + 128);
+            const Half fs = {*(const uint4 *)(here + so), *(const uint4 *)(here + (so ^ 32))};
+#pragma unroll
+            for (int i = 0; i < FR; ++i) {
+                const Half fr = {*(const uint4 *)(here + ro + i * 2048), *(const uint4 *)(here + (ro ^ 32) + i * 2048)};
+                if (KK == 0) p[i] = f32x16{};
+                product_of<CLOSE>(fr, fs, p[i]);
+            }
+            stage = stage + 1 < STAGES ? stage + 1 : 0;
+        };
+        auto add = [&] {
+#pragma unroll
+            for (int i = 0; i < FR; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][e] = fmaf(p[i][e], s, acc[i][e]);
+        };
+        int k = 0;
+        for (; k + 2 <= steps; k += 2) {
+            step(std::integral_constant<int, 0>(), k);
+            step(std::integral_constant<int, 1>(), k + 1);
+            add();
+        }
+        if (k < steps) {                                         // (a last block of one step)
+            step(std::integral_constant<int, 0>(), k);
+            add();
+        }
+        const int free_stage = (stage + 2) & 3;                  // the last step's but one
+        static_assert(STAGES == 4, "stages in turn");
+        const int r1 = r0 + wr * FR * 32, s1 = s0 + wsv * 32;
+        if constexpr (SPLIT) {
+            float *const part = a.part + (int64_t)range * a.T * a.O;
+            const int t = s1 + l32;
+#pragma unroll
+            for (int i = 0; i < FR; ++i) {
+                const int o = r1 + i * 32 + 4 * half;
+                if (t >= a.T) continue;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float v[4] = {acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
+                    if (o + 8 * q < a.O) store_piece<float, 4>(part + (int64_t)t * a.O + o + 8 * q, a.O - o - 8 * q, v);
+                }
+            }
+            fetch(free_stage);
+            continue;
+        }
+        // All of it inside y, in one sequence and one part of y: places are linear in rows and columns.
+        bool whole = sizeof(T) == 2 && r0 + BR <= a.O && s0 + BS <= a.T && (CHANNELS ? a.N : a.O) < 1 << 26;       // (32-bit distances of fifteen rows)
+        if (CHANNELS)
+            whole = whole && quotient(s0, a.N, a.by_n) == quotient(s0 + BS - 1, a.N, a.by_n) &&
+                    quotient(r0, a.per_part, a.by_part) == quotient(r0 + BR - 1, a.per_part, a.by_part);
+        bool done = false;
+        if constexpr (sizeof(T) == 2) {
+            if (whole) {
+                done = true;
+                // The stage of the last step but one: every wave has read it, and what comes there next is, in a wave's own 2 KB, that wave's own transfers. The bias
+                // is there three steps after it was asked for; with fewer steps it is waited for.
+                if (steps < 4) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                char *const mine = lds + free_stage * STAGE + wave * 2048;
+                const float *const bias = (const float *)(own + STAGES * 256);
+                const uint32_t stride = CHANNELS ? (uint32_t)a.N : (uint32_t)a.O;
+                const char *const y = uniform((const char *)((T *)a.y + token_of(a, s1) + output_of(a, r1)));
+                const uint32_t at = ((uint32_t)(lane >> 2) * stride + (lane & 3) * 8) * 2u;
+#pragma unroll
+                for (int i = 0; i < FR; ++i) {
+                    if constexpr (CHANNELS) channels_to_lds<T, 32>(mine, acc[i], 0, bias + i * 32);
+                    else tokens_to_lds<T, 64>(mine, acc[i], 0, bias + i * 32);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const uint4 v = CHANNELS ? output_piece<32>(mine, t) : token_piece<64>(mine, t);
+                        const int64_t place = CHANNELS ? (int64_t)(i * 32 + 16 * t) * stride : (int64_t)(16 * t) * stride + i * 32;
+                        put16<false>((char *)y + place * 2 + at, v);
+                    }
+                }
+            }
+        }
+        if (!done) {
+            const int t = s1 + l32;
+            const int64_t token = token_of(a, min(t, a.T - 1));
+#pragma unroll
+            for (int i = 0; i < FR; ++i) store_f8<T>(a, acc[i], r1 + i * 32, t, token);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(free_stage);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // nothing is on its way to LDS when the workgroup ends
 }
@@ -606,32 +740,31 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
             return FFTCONV_OK;
         });
     };
-    auto launch_async = [&](auto fr, auto fs, auto split) -> int {
-        constexpr int FR = decltype(fr)::value, FS = decltype(fs)::value, BR = 64 * FR, BS = 128 * FS, lds = 2 * (BR + BS) * 128 + 8 * (2 * 512 + FR * 128);
-        constexpr bool SPLIT = decltype(split)::value;
-        a.tiles_r = (a.O + BR - 1) / BR, a.tiles_s = (a.T + BS - 1) / BS;
+    auto launch_async = [&](auto kernel, int block, int lds, int most) -> int {
+        a.tiles_r = (a.O + block - 1) / block, a.tiles_s = (a.T + block - 1) / block;
         const Walk w = {a.tiles_s, a.tiles_s <= 12 ? a.tiles_s : 8, a.tiles_r * a.tiles_s * a.ranges};
-        const auto kernel = a.channels && !SPLIT ? k_f8_async<T, !SPLIT, SPLIT, FR, FS> : k_f8_async<T, false, SPLIT, FR, FS>;
         FC_TRY(raise_dynamic_lds((const void *)kernel, lds));
-        const int most = 256 * (FR == 4 ? 1 : 2);
         kernel<<<(unsigned)(w.tiles < most ? w.tiles : most), 512, lds, s>>>(a, w);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     };
+    constexpr int LARGE_LDS = 2 * 512 * 128 + 8 * (2 * 512 + 512), SMALL_LDS = 4 * 256 * 64 + 8 * (4 * 256 + 256);
     auto tiles = [&](int64_t b) { return ((a.O + b - 1) / b) * ((a.T + b - 1) / b); };
     const bool pieces = a.K % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.w) % 16 == 0;
     using std::integral_constant;
     a.ranges = f8_ranges(a.T, a.K, a.O);
     if (pieces && a.ranges > 1) {
         a.per = (a.blocks + a.ranges - 1) / a.ranges, a.part = (float *)workspace;
-        FC_TRY(launch_async(integral_constant<int, 2>(), integral_constant<int, 1>(), std::true_type()));
+        FC_TRY(launch_async(k_f8_small<T, false, true>, 128, SMALL_LDS, 512));
         k_f8_sums<T><<<(unsigned)(((int64_t)a.T * a.O + 1023) / 1024), 256, 0, s>>>(a);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
     }
     a.ranges = 1;
-    if (pieces && tiles(256) >= 256) return launch_async(integral_constant<int, 4>(), integral_constant<int, 2>(), std::false_type());
-    if (pieces && tiles(128) >= 128) return launch_async(integral_constant<int, 2>(), integral_constant<int, 1>(), std::false_type());
+    if constexpr (sizeof(T) == 2) {
+        if (pieces && tiles(256) >= 256) return a.channels ? launch_async(k_f8_large<T, true>, 256, LARGE_LDS, 256) : launch_async(k_f8_large<T, false>, 256, LARGE_LDS, 256);
+    }
+    if (pieces && tiles(128) >= 128) return a.channels ? launch_async(k_f8_small<T, true, false>, 128, SMALL_LDS, 512) : launch_async(k_f8_small<T, false, false>, 128, SMALL_LDS, 512);
     if (tiles(128) >= 256) return launch(integral_constant<int, 2>());
     return launch(integral_constant<int, 1>());
 }

@@ -53,10 +53,6 @@ template <int FR, int FS> struct Tile {
     static constexpr int STAGE = (BR + BS) * BK;
 };
 
-// The place in LDS of 16-byte piece c (0 .. 3) of a 64-byte row. A clock delivers 256 bytes, here the same piece of sixteen rows in a run: four rows
-// lie in 256 bytes, so the piece is moved by the row's number above that, and all sixteen come from banks of their own.
-__device__ __forceinline__ int piece_at(int row, int c) { return row * 64 + ((c ^ ((row >> 2) & 3)) << 4); }
-
 __device__ __forceinline__ i32x16 mfma_i8(uint4 a, uint4 b, i32x16 c)
 {
     return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
