@@ -9,7 +9,8 @@
 // exchanges inside the vector unit, the four rows of a wave one after the other with what comes in), and each walks its samples once more from
 // what the lanes before it leave. A wave takes 512 samples of a row at a time, eight in a run for each lane; short rows get part of a wave.
 // Everything between the load of u, w, v (and dy) and the store of y (du, dw, dv) is fp32 in registers: every tensor moves once, and that is what
-// bounds these kernels.
+// bounds these kernels: bf16 64 x 768 x 4096 forward 296 us, 5.4 TB/s, backward 527 us, 5.3 TB/s. What comes next is asked for before the samples in
+// hand are worked on: 1024 rows of 65536 164 and 202 us, without 261 and 364.
 //
 // Few rows: a row goes in segments to waves of their own. A first kernel composes each segment to one map, and every wave of the second applies
 // those before its own to the row's state (gradients: those behind it to `dlast`).
@@ -128,20 +129,36 @@ template <bool REVERSE, int G> __device__ __forceinline__ float into_lane(Map m,
     }
 }
 
-// What a wave's lanes have of G lanes' samples from `col` on: gates and inputs of samples below `len`; behind it the state stays what it is.
-template <typename T, bool WHOLE> struct Piece {
-    float a[SE], rest[SE], u[SE], x[SE];
-    __device__ __forceinline__ void load(const ScanArgs &g, int64_t row, int64_t col, int64_t len, bool all)
+// Eight samples of a lane as they lie in memory, zeros where a row has ended: what is asked for while the 512 samples before are worked on.
+template <typename T> struct Raw {
+    T v[SE];
+    template <bool WHOLE> __device__ __forceinline__ void load(const void *p, int64_t row, int64_t col, int64_t N)
     {
-        float w[SE];
-        load_row_piece<T, SE, WHOLE>((const T *)g.u + row * g.N, col, g.N, u);
-        load_row_piece<T, SE, WHOLE>((const T *)g.w + row * g.N, col, g.N, w);
-        if (g.log_gate) {
-#pragma unroll
-            for (int e = 0; e < SE; ++e) gate_of<T>(w[e], true, a[e], rest[e]), x[e] = u[e];
+        const T *const x = (const T *)p + row * N;
+        if constexpr (WHOLE) {                                   // (a piece that is not there is read at the row's beginning: no branch parts the loads)
+            load_bytes<SE * (int)sizeof(T)>(x + (col < N ? col : 0), v);
+        } else if (col + SE <= N) {
+            load_bytes<SE * (int)sizeof(T)>(x + col, v);
         } else {
 #pragma unroll
-            for (int e = 0; e < SE; ++e) gate_of<T>(w[e], false, a[e], rest[e]), x[e] = rest[e] * u[e];
+            for (int e = 0; e < SE; ++e) v[e] = col + e < N ? x[col + e] : (T)0.f;
+        }
+    }
+};
+
+// What a wave's lanes have of G lanes' samples from `col` on: gates and inputs of samples below `len`; behind it the state stays what it is.
+template <typename T> struct Piece {
+    float a[SE], rest[SE], u[SE], x[SE];
+    __device__ __forceinline__ void take(const ScanArgs &g, const Raw<T> &ru, const Raw<T> &rw, int64_t col, int64_t len, bool all)
+    {
+#pragma unroll
+        for (int e = 0; e < SE; ++e) u[e] = to_f32(ru.v[e]);
+        if (g.log_gate) {
+#pragma unroll
+            for (int e = 0; e < SE; ++e) gate_of<T>(to_f32(rw.v[e]), true, a[e], rest[e]), x[e] = u[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < SE; ++e) gate_of<T>(to_f32(rw.v[e]), false, a[e], rest[e]), x[e] = rest[e] * u[e];
         }
         if (!all) {
 #pragma unroll
@@ -205,20 +222,29 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
         if (seg > 0) h = through_segments<false>(g.maps + row * g.segments, 0, seg, h);
     }
     const int end = min((seg + 1) * g.per, g.chunks);
+    Raw<T> u, w, v;
+    auto ask = [&](int k) {
+        const int64_t begin = (int64_t)k * (G * SE), col = begin + lane * SE;
+        if (k >= end || begin >= len) return;
+        u.template load<WHOLE>(g.u, row, col, g.N);
+        w.template load<WHOLE>(g.w, row, col, g.N);
+        if (g.v) v.template load<WHOLE>(g.v, row, col, g.N);
+    };
+    ask(seg * g.per);
     for (int k = seg * g.per; k < end; ++k) {
         const int64_t begin = (int64_t)k * (G * SE), col = begin + lane * SE;
         if (g.kept && lane == 0 && there) g.kept[row * g.chunks + k] = h;
         T y[SE] = {};
         if (begin < len) {
-            Piece<T, WHOLE> p;
-            p.load(g, row, col, len, begin + G * SE <= len);
-            float v[SE];
-            if (g.v) load_row_piece<T, SE, WHOLE>((const T *)g.v + row * g.N, col, g.N, v);
+            Piece<T> p;
+            p.take(g, u, w, col, len, begin + G * SE <= len);
+            const Raw<T> gate = v;
+            ask(k + 1);
             float s = into_lane<false, G>(p.map(), h);
 #pragma unroll
             for (int e = 0; e < SE; ++e) {
                 s = fmaf(p.a[e], s, p.x[e]);
-                const float o = g.v ? s * v[e] : s;
+                const float o = g.v ? s * to_f32(gate.v[e]) : s;
                 y[e] = from_f32<T>(col + e < len ? o : 0.f);
             }
         }
@@ -247,8 +273,11 @@ template <typename T, bool BACK, bool WHOLE> __global__ void __launch_bounds__(2
         const bool all = at + 64 * SE <= len;
         Map own;
         if constexpr (!BACK) {
-            Piece<T, WHOLE> p;
-            p.load(g, row, col, len, all);
+            Raw<T> u, w;
+            u.template load<WHOLE>(g.u, row, col, g.N);
+            w.template load<WHOLE>(g.w, row, col, g.N);
+            Piece<T> p;
+            p.take(g, u, w, col, len, all);
             own = p.map();
         } else {
             float w[SE], dy[SE], v[SE];
@@ -298,23 +327,34 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
         if (seg < g.segments - 1) p = through_segments<true>(g.maps + row * g.segments, seg + 1, g.segments - 1 - seg, p);
     }
     const int first = seg * g.per;
-    for (int k = min((seg + 1) * g.per, g.chunks) - 1; k >= first; --k) {
+    Raw<T> ru, rw, rv, rdy;
+    float kept = 0.f;
+    auto ask = [&](int k) {
+        const int64_t begin = (int64_t)k * (G * SE), col = begin + lane * SE;
+        if (k < first || begin >= len) return;
+        ru.template load<WHOLE>(g.u, row, col, g.N);
+        rw.template load<WHOLE>(g.w, row, col, g.N);
+        rdy.template load<WHOLE>(g.dy, row, col, g.N);
+        if (g.v) rv.template load<WHOLE>(g.v, row, col, g.N);
+        kept = g.kept_in[row * g.chunks + k];
+    };
+    const int top = min((seg + 1) * g.per, g.chunks) - 1;
+    ask(top);
+    for (int k = top; k >= first; --k) {
         const int64_t begin = (int64_t)k * (G * SE), col = begin + lane * SE;
         T du[SE] = {}, dw[SE] = {}, dv[SE] = {};
         if (begin < len) {
             const bool all = begin + G * SE <= len;
-            Piece<T, WHOLE> q;
-            float w[SE], dy[SE], v[SE];
-            load_row_piece<T, SE, WHOLE>((const T *)g.dy + row * g.N, col, g.N, dy);
-            if (g.v) load_row_piece<T, SE, WHOLE>((const T *)g.v + row * g.N, col, g.N, v);
-            q.load(g, row, col, len, all);
-            if (g.log_gate) load_row_piece<T, SE, WHOLE>((const T *)g.w + row * g.N, col, g.N, w);
-            float h = g.kept_in[row * g.chunks + k], d[SE];
+            Piece<T> q;
+            q.take(g, ru, rw, col, len, all);
+            const Raw<T> w = rw, dy = rdy, v = rv;
+            float h = kept, d[SE];
+            ask(k - 1);
             float s = into_lane<false, G>(q.map(), h);
             Map m = {1.f, 0.f};
 #pragma unroll
             for (int e = SE - 1; e >= 0; --e) {
-                d[e] = g.v ? dy[e] * v[e] : dy[e];
+                d[e] = g.v ? to_f32(dy.v[e]) * to_f32(v.v[e]) : to_f32(dy.v[e]);
                 if (!all) d[e] = col + e < len ? d[e] : 0.f;
                 m.x = q.a[e] * (d[e] + m.x);
                 m.a *= q.a[e];
@@ -332,7 +372,7 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
                 float gu, gw;
                 if (g.log_gate) {
                     gu = d[e];
-                    gw = w[e] > 0.f ? 0.f : d[e] * before * q.a[e];
+                    gw = to_f32(w.v[e]) > 0.f ? 0.f : d[e] * before * q.a[e];
                 } else {
                     gu = d[e] * q.rest[e];
                     gw = d[e] * (before - q.u[e]) * (q.a[e] * q.rest[e]);
@@ -340,8 +380,10 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
                 const bool in = all || col + e < len;
                 du[e] = from_f32<T>(in ? gu : 0.f);
                 dw[e] = from_f32<T>(in ? gw : 0.f);
-                dv[e] = from_f32<T>(in ? dy[e] * s : 0.f);
+                dv[e] = from_f32<T>(in ? to_f32(dy.v[e]) * s : 0.f);
             }
+        } else {
+            ask(k - 1);
         }
         if (there && (!WHOLE || col < g.N)) {
             const int64_t at = row * g.N + col, left = WHOLE ? SE : g.N - col;
@@ -375,11 +417,15 @@ template <typename T> __global__ void __launch_bounds__(256) k_step(const StepAr
     ((T *)g.y)[i] = from_f32<T>(g.v ? h * to_f32(((const T *)g.v)[i]) : h);
 }
 
-// Into how many segments a row goes: none where there are 16 waves for every compute unit (4096 rows), else as many as bring 32.
+// Into how many segments a row goes. A wave takes about 0.9 us for 512 samples (gradients 1.4) however few waves there are; a second kernel costs 2.5 us and
+// reads u and w (w, v and dy) again. bf16, forward and backward in us: 500 rows of 2048 in one 5.9 and 7.9, in four 7.8 and 8.8; of 4096 9.1 and
+// 13.6, in eight 9.2 and 12.2; of 8192 17 and 24, 13.7 and 19; 1024 rows of 16384 32 and 50, in eight 37 and 55; 256 rows of 4096 8.9 and 13.4, 8.0 and 9.1;
+// 16 rows of 65536 110 and 173, in 128 7.9 and 9.5. So: rows of more than 2048 samples, fewer than 1024 of them, and no more than 64 for each 512
+// samples, in as many segments as bring 32 waves to a compute unit.
 static int scan_segments(int64_t rows, int64_t N)
 {
     const int64_t chunks = (N + 64 * SE - 1) / (64 * SE);
-    if (rows < 1 || rows >= 4096 || chunks < 2) return 1;
+    if (rows < 1 || rows >= 1024 || chunks <= 4 || chunks * 64 < rows) return 1;
     const int64_t most = (8192 + rows - 1) / rows, per = most < chunks ? (chunks + most - 1) / most : 1;
     return (int)((chunks + per - 1) / per);
 }
