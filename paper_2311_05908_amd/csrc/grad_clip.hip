@@ -25,26 +25,21 @@ struct Tensors {
 };
 
 struct ClipArgs {
-    double *sums;                                // a workgroup's each
-    const double *total;                         // the norm, or
+    double *sums;                                // of the workgroups of the first pass, one each
+    double *total;                               // the norm
     const float *norm;                           // one that came with the call
+    float *norm_out;
     double limit, eps;
-    uint32_t per;                                // pieces of a workgroup
+    int64_t count;                               // sums, where the second pass adds them up itself
 };
 
-// f(tensor, first value, values) for the pieces from `begin` up to `end`, or the other way about.
-template <bool DOWN, typename F> __device__ __forceinline__ void each_piece(const Tensors &t, uint32_t begin, uint32_t end, F f)
+// f(tensor, first value, values) for this workgroup's pieces: every gridDim.x'th, from the first on, or with DOWN from the last.
+template <bool DOWN, typename F> __device__ __forceinline__ void each_piece(const Tensors &t, F f)
 {
-    if (begin >= end) return;
-    const uint32_t at0 = DOWN ? end - 1 : begin;
-    int lo = 0, hi = t.n - 1;                    // the last tensor that starts at or before it
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (t.start[mid] <= at0) lo = mid;
-        else hi = mid - 1;
-    }
-    for (uint32_t i = 0; i < end - begin; ++i) {
-        const uint32_t at = DOWN ? end - 1 - i : begin + i;
+    const uint32_t all = t.start[t.n];
+    int lo = DOWN ? t.n - 1 : 0;
+    for (uint32_t i = blockIdx.x; i < all; i += gridDim.x) {
+        const uint32_t at = DOWN ? all - 1 - i : i;
         if (DOWN) while (t.start[lo] > at) --lo;
         else while (t.start[lo + 1] <= at) ++lo;
         const int64_t first = (int64_t)(at - t.start[lo]) * PIECE, left = t.count[lo] - first;
@@ -67,42 +62,43 @@ template <typename T> __device__ __forceinline__ void add_squares(const void *p,
         for (int e = 0; e < 8; ++e) sum = fma((double)v[i][e], (double)v[i][e], sum);
 }
 
-// The workgroup's sum, in thread 0.
-template <int THREADS> __device__ __forceinline__ double group_sum(double x)
+// The workgroup's sum, in every thread.
+__device__ __forceinline__ double group_sum(double x)
 {
-    __shared__ double part[THREADS / 64];
+    __shared__ double part[4];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
-    if (threadIdx.x == 0)
-        for (int i = 1; i < THREADS / 64; ++i) x += part[i];
-    return x;
+    return part[0] + part[1] + part[2] + part[3];
+}
+__device__ __forceinline__ double norm_of(const double *sums, int64_t n)
+{
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 256) sum += sums[i];
+    return sqrt(group_sum(sum));
 }
 
 __global__ void __launch_bounds__(256) k_squares(const Tensors t, const ClipArgs a)
 {
     static_assert(PIECE == 256 * 32, "four times eight values to a thread");
     double sum = 0.0;
-    const uint32_t begin = blockIdx.x * a.per, all = t.start[t.n];
-    each_piece<false>(t, begin, min(begin + a.per, all), [&](int i, int64_t first, int count) {
+    each_piece<false>(t, [&](int i, int64_t first, int count) {
         const int type = t.type[i] & 3;
         if (type == FFTCONV_F32) add_squares<float>(t.in[i], first, count, sum);
         else if (type == FFTCONV_F16) add_squares<_Float16>(t.in[i], first, count, sum);
         else add_squares<__bf16>(t.in[i], first, count, sum);
     });
-    sum = group_sum<256>(sum);
+    sum = group_sum(sum);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = sum;
 }
 
-__global__ void __launch_bounds__(1024) k_norm(const double *sums, int64_t n, double *total, float *norm)
+__global__ void __launch_bounds__(256) k_norm(const ClipArgs a)
 {
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 1024) sum += sums[i];
-    sum = sqrt(group_sum<1024>(sum));
+    const double norm = norm_of(a.sums, a.count);
     if (threadIdx.x == 0) {
-        *total = sum;
-        if (norm) *norm = (float)sum;
+        *a.total = norm;
+        if (a.norm_out) *a.norm_out = (float)norm;
     }
 }
 
@@ -127,10 +123,11 @@ template <typename T, typename O> __device__ __forceinline__ void scale_piece(co
 
 __global__ void __launch_bounds__(256) k_clip(const Tensors t, const ClipArgs a)
 {
-    const double c = a.limit / ((a.norm ? (double)*a.norm : *a.total) + a.eps);
+    const double norm = a.norm ? (double)*a.norm : a.count ? norm_of(a.sums, a.count) : *a.total;
+    if (a.norm_out && blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
+    const double c = a.limit / (norm + a.eps);
     const float by = c > 1.0 ? 1.f : (float)c;   // (a norm that is no number makes everything so)
-    const uint32_t begin = blockIdx.x * a.per, all = t.start[t.n];
-    each_piece<true>(t, begin, min(begin + a.per, all), [&](int i, int64_t first, int count) {
+    each_piece<true>(t, [&](int i, int64_t first, int count) {
         const int type = t.type[i] & 3;
         const bool wide = t.type[i] >> 2 == FFTCONV_F32;
         if (by == 1.f && t.in[i] == t.out[i]) return;
@@ -142,7 +139,7 @@ __global__ void __launch_bounds__(256) k_clip(const Tensors t, const ClipArgs a)
     });
 }
 
-// The launches of a call: f(tensors, workgroups, pieces of one), one after the other, from the last with `down`, until one returns a code.
+// The launches of a call: f(tensors, workgroups), one after the other, from the last with `down`, until one returns a code.
 template <typename F> static int each_launch(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out,
                                              int64_t tensors, bool down, F f)
 {
@@ -161,8 +158,7 @@ template <typename F> static int each_launch(const void *const *in, void *const 
         }
         t.start[t.n] = pieces;
         if (t.n == 0) continue;
-        const uint32_t most = 2048, per = (pieces + most - 1) / most, groups = (pieces + per - 1) / per;
-        if (const int rc = f(t, groups, per)) return rc;
+        if (const int rc = f(t, pieces < 2048 ? pieces : 2048u)) return rc;
     }
     return FFTCONV_OK;
 }
@@ -170,7 +166,7 @@ template <typename F> static int each_launch(const void *const *in, void *const 
 size_t clip_workspace(const int64_t *counts, int64_t tensors)
 {
     size_t n = 1;
-    (void)each_launch(nullptr, nullptr, counts, nullptr, nullptr, tensors, false, [&](const Tensors &, uint32_t groups, uint32_t) { n += groups; return FFTCONV_OK; });
+    (void)each_launch(nullptr, nullptr, counts, nullptr, nullptr, tensors, false, [&](const Tensors &, uint32_t groups) { n += groups; return FFTCONV_OK; });
     return n * sizeof(double);
 }
 
@@ -213,22 +209,26 @@ int clip_overlaps(const void *const *in, void *const *out, const int64_t *counts
 int clip_grads(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors, double limit,
                double eps, const float *norm_in, float *norm, void *workspace, hipStream_t s)
 {
+    // (up to 512 sums are added up by every workgroup of the second pass, and a launch is saved)
     double *const total = (double *)workspace;
-    ClipArgs a = {total ? total + 1 : nullptr, total, norm_in, limit, eps, 0};
+    ClipArgs a = {total ? total + 1 : nullptr, total, norm_in, nullptr, limit, eps, 0};
     if (!norm_in) {
-        FC_TRY(each_launch(in, nullptr, counts, types, nullptr, tensors, false, [&](const Tensors &t, uint32_t groups, uint32_t per) -> int {
-            a.per = per;
+        int64_t sums = 0;
+        FC_TRY(each_launch(in, nullptr, counts, types, nullptr, tensors, false, [&](const Tensors &t, uint32_t groups) -> int {
             k_squares<<<groups, 256, 0, s>>>(t, a);
             FC_HIP(hipGetLastError());
-            a.sums += groups;
+            a.sums += groups, sums += groups;
             return FFTCONV_OK;
         }));
-        k_norm<<<1, 1024, 0, s>>>(total + 1, a.sums - (total + 1), total, norm);
-        FC_HIP(hipGetLastError());
+        a.sums = total + 1, a.count = sums, a.norm_out = norm;
+        if (!out || sums == 0 || sums > 512) {
+            k_norm<<<1, 256, 0, s>>>(a);
+            FC_HIP(hipGetLastError());
+            a.count = 0, a.norm_out = nullptr;
+        }
     }
     if (!out) return FFTCONV_OK;
-    return each_launch(in, out, counts, types, types_out, tensors, true, [&](const Tensors &t, uint32_t groups, uint32_t per) -> int {
-        a.per = per;
+    return each_launch(in, out, counts, types, types_out, tensors, true, [&](const Tensors &t, uint32_t groups) -> int {
         k_clip<<<groups, 256, 0, s>>>(t, a);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
