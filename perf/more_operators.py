@@ -235,7 +235,7 @@ def _run_own(s, c, dtype):
         (q, scale), (qt, _) = layers.quantize_tiles(s["w"], transposed=True)
         return {"q": q, "scale": scale, "qt": qt}
     if op == "linear back":
-        rows = layers.quantize_blocks(s["x"], layout="channels", parts=c["parts"])
+        rows = layers.quantize_blocks(s["x"] if c["parts"] > 1 else s["x"][0], layout="channels", parts=c["parts"])
     else:
         rows = layers.quantize_blocks(s["x"])
     return {"y": layers.linear_f8(rows, (s["wq"], s["ws"]), bias=s["bias"], dtype=dtype, layout=c["layout"], parts=c["parts"] if op == "linear" else 1)}
