@@ -1,0 +1,126 @@
+"""examples/recurrent_layer.py: the norm, the projections in 8-bit floating point, the recurrence and the clipping together, against the layer in 64 bits
+without any 8-bit rounding.
+
+The bounds: e4m3 has three bits behind the first, steps of an eighth of a number's power of two, so a value is off by 1 / 8 / sqrt(12) / 1.5, 2.4 % of
+itself as a root mean square. A result here has at most ten such values in a chain of products (two a projection, and through u, w and v three times
+those of the first): sqrt(10) 2.4 % = 7.6 %, and bf16's and the checkpoints' roundings, 1.4 %, in their squares 8 %: 10 % of the result's root mean square."""
+import importlib.util
+import os
+
+import pytest
+import torch
+
+from paper_2311_05908_amd import layers
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def example():
+    spec = importlib.util.spec_from_file_location("recurrent_layer", os.path.join(ROOT, "examples", "recurrent_layer.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def plain(x, r, norm, w_in, b_in, w_out):
+    """out (b, n, d), h, and the state after the last sample, in 64 bits."""
+    h = x + r
+    z = h / torch.sqrt((h * h).mean(-1, keepdim=True) + 1e-6) * norm
+    u, w, v = (z @ w_in.T + b_in).chunk(3, -1)
+    a = torch.sigmoid(w)
+    s, ss = torch.zeros_like(u[:, 0]), []
+    for t in range(x.shape[1]):
+        s = a[:, t] * s + (1 - a[:, t]) * u[:, t]
+        ss.append(s)
+    return (v * torch.stack(ss, 1)) @ w_out.T, h, s
+
+
+def off(a, b):
+    return float((a.double() - b).norm() / b.norm())
+
+
+@pytest.mark.parametrize("batch,samples,channels", [(3, 300, 96), (2, 700, 256), (1, 129, 200)])
+def test_layer(batch, samples, channels):
+    layer = example().RecurrentLayer(channels, seed=samples)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, r, dout, dh = (torch.randn(batch, samples, channels, generator=g, device="cuda").to(layer.dtype) for _ in range(4))
+    leaves = [t.double().requires_grad_(True) for t in (x, r, layer.norm, layer.w_in, layer.b_in, layer.w_out)]
+    want, h, s = plain(*leaves)
+    ((want * dout.double()).sum() + (h * dh.double()).sum()).backward()
+    out, hg, kept = layer.train_forward(x, r)
+    assert off(out, want.detach()) < 0.1 and off(hg, h.detach()) < 0.004
+    dx, grads = layer.backward(kept, dout, dh=dh)
+    for name, a, b in (("dx", dx, leaves[0]), *zip(("dnorm", "dw_in", "db_in", "dw_out"), grads, leaves[2:])):
+        print(name, off(a, b.grad))
+        assert torch.isfinite(a.float()).all() and off(a, b.grad) < 0.1, name
+    again, _, state = layer.forward(x, r)
+    assert torch.equal(again, out) and off(state, s.detach()) < 0.1
+
+
+def test_prompts_of_their_own_lengths_and_tokens_after_them():
+    """A padded batch and steps after it: what each sequence gives alone, as one prompt. (Sums of the recurrence are made in another order, so y may be a bf16 step
+    off, and what is quantised from it an eighth: a difference of 2^-3 in few values, far below the 10 % of the whole that is asked for.)"""
+    layer = example().RecurrentLayer(160, seed=3)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n, more = 200, 4
+    ends = [200, 1, 77]
+    x, r = (torch.randn(3, n + more, 160, generator=g, device="cuda").to(layer.dtype) for _ in range(2))
+    px, pr = x[:, :n].clone(), r[:, :n].clone()
+    for i, end in enumerate(ends):
+        px[i, end:] = float("nan")               # what lies behind a sequence is not used
+        pr[i, end:] = 0
+    lengths = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    out, _, state = layer.forward(px, pr, lengths=lengths)
+    alone = [layer.forward(x[i:i + 1, :end + more].contiguous(), r[i:i + 1, :end + more].contiguous()) for i, end in enumerate(ends)]
+    for i, end in enumerate(ends):
+        assert off(out[i, :end], alone[i][0][0, :end].double()) < 0.1
+    for t in range(more):
+        tx, tr = (torch.stack([a[i, end + t] for i, end in enumerate(ends)]) for a in (x, r))
+        y, h = layer.step(tx, tr, state)
+        assert torch.equal(h, (tx.float() + tr.float()).to(h.dtype))
+        for i, end in enumerate(ends):
+            assert off(y[i], alone[i][0][0, end + t].double()) < 0.1
+    for i in range(3):
+        assert off(state[i], alone[i][2][0].double()) < 0.1
+
+
+def test_update_clips():
+    layer = example().RecurrentLayer(64, seed=5)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, r, dout = (torch.randn(2, 50, 64, generator=g, device="cuda").to(layer.dtype) for _ in range(3))
+    _, _, kept = layer.train_forward(x, r)
+    _, grads = layer.backward(kept, dout)
+    was = [t.clone() for t in (layer.norm, layer.w_in, layer.b_in, layer.w_out)]
+    norm = float(torch.stack([t.double().square().sum() for t in grads]).sum().sqrt())
+    before = [t.clone() for t in grads]
+    got = layer.update(grads, 0.5, limit=norm / 4)
+    assert abs(float(got) - norm) <= 2.0 ** -23 * norm
+    for p, w, t, b in zip((layer.norm, layer.w_in, layer.b_in, layer.w_out), was, grads, before):
+        # factor and product rounded: 3 half steps of the value; the addition one of the sum
+        want = w.double() - 0.5 * b.double() * min(1.0, norm / 4 / (norm + 1e-6))
+        assert bool(((p.double() - want).abs() <= 4 * 2.0 ** -24 * (b.double().abs() + want.abs())).all())
+    assert torch.equal(layers.quantize_tiles(layer.w_in).q.view(torch.uint8), layer.in8.q.view(torch.uint8))
+
+
+def test_a_step_in_a_graph():
+    """A captured token step, replayed over new tokens with the state going on in place."""
+    layer = example().RecurrentLayer(128, seed=6)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, r = (torch.randn(6, 2, 128, generator=g, device="cuda").to(layer.dtype) for _ in range(2))
+    state = torch.randn(2, 128, generator=g, device="cuda")
+    want, s = [], state.clone()
+    for t in range(6):
+        want.append((layer.step(x[t], r[t], s)[0], s.clone()))
+    tx, tr, s = torch.empty_like(x[0]), torch.empty_like(r[0]), state.clone()
+    tx.copy_(x[0]), tr.copy_(r[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, _ = layer.step(tx, tr, s)
+    s.copy_(state)
+    for t in range(6):
+        tx.copy_(x[t]), tr.copy_(r[t])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[t][0]) and torch.equal(s, want[t][1])
+        layer.step(x[0], r[0], torch.zeros_like(s))
