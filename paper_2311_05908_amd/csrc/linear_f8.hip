@@ -260,6 +260,12 @@ template <int WIDE> __device__ __forceinline__ uint4 output_piece(const char *ow
 // The same for operands in pieces of 16 bytes (K a multiple of 16): 2 x 4 waves, pieces straight to LDS, a block of 128 while the one before it is
 // multiplied, in one stream over a workgroup's tiles. A wave holds the tokens' operands of a block and brings the weight's 32 rows at a time, one group
 // ahead; sums of a block are two accumulators in turn, added to the totals while the next products run.
+//
+// Measured: f16 8192 x 4096 -> 16384 583 us, 1.9 PFLOP/s; bf16 64 x 4096 x 2304 -> 768 547 us, 1.7. The socket is at its cap back to back (1395 and 1399 of
+// 1400 W), so joules count: the products with their reads of LDS alone take 327 us, the scales' multiply-adds 110 on top, what is brought 100, what is
+// stored 80. (The library's product with one scale for each operand: 479 us on these values at the same cap.) Hence the large tile, whole lines to a
+// store, and one multiply-add for a value and block. Bringing blocks a block and a half ahead, in two parts, 617 us; storing a tile's results among the next
+// one's first products 722, for registers then go to memory; other orders of the tiles 569 to 620.
 template <typename T, bool CHANNELS> __global__ void __launch_bounds__(512, 2) k_f8_large(const F8Args a, const Walk walk)
 {
     constexpr int FR = 4, FS = 2, BR = 64 * FR, BS = 128 * FS, STAGE = (BR + BS) * 128, LI = (BR + BS) / 64;
@@ -451,8 +457,9 @@ template <typename T, bool CHANNELS> __global__ void __launch_bounds__(512, 2) k
 
 // Tiles of 128 x 128, where there are too few of 256 x 256: 2 x 4 waves of 64 outputs by 32 tokens, four steps of 64 of k in LDS, asked for three steps ahead,
 // for here it is how long a transfer takes that counts (4096 x 768 -> 2304: six blocks to a tile). Sums of a block stay in their accumulators over its two
-// steps. Two workgroups share a compute unit.
-template <typename T, bool CHANNELS, bool SPLIT> __global__ void __launch_bounds__(512, 4) k_f8_small(const F8Args a, const Walk walk)
+// steps. Two workgroups share a compute unit, and one reads its operands while the other multiplies; ALONE, where there is a unit for every tile, a
+// wave's own operands are read a step ahead, and its pieces asked for four ahead.
+template <typename T, bool CHANNELS, bool SPLIT, bool ALONE> __global__ void __launch_bounds__(512, ALONE ? 2 : 4) k_f8_small(const F8Args a, const Walk walk)
 {
     constexpr int FR = 2, BR = 128, BS = 128, BK = 64, STAGE = (BR + BS) * BK, STAGES = 4;
     constexpr bool CLOSE = sizeof(T) == 4;
@@ -520,11 +527,20 @@ template <typename T, bool CHANNELS, bool SPLIT> __global__ void __launch_bounds
 
     if (first >= last) return;
     aim();
-    fetch(0);
-    fetch(1);
-    fetch(2);
+#pragma unroll
+    for (int i = 0; i < (ALONE ? STAGES : STAGES - 1); ++i) fetch(i);
     // where this lane's pieces are, from a stage's start: half of a row's, and the other two at ^ 32
     const int ro = piece_at(wr * FR * 32 + l32, half), so = BR * BK + piece_at(wsv * 32 + l32, half);
+    Half fr[2][FR], fs[2];
+    auto read = [&](int buf, const char *here) {
+#pragma unroll
+        for (int i = 0; i < FR; ++i) fr[buf][i] = {*(const uint4 *)(here + ro + i * 2048), *(const uint4 *)(here + (ro ^ 32) + i * 2048)};
+        fs[buf] = {*(const uint4 *)(here + so), *(const uint4 *)(here + (so ^ 32))};
+    };
+    if constexpr (ALONE) {
+        FC_ARRIVED(2 + 3 + 2);                                   // three transfers with a block's first step, two with its second
+        read(0, lds);
+    }
     int stage = 0;
     for (int tile = first; tile < last; tile += on_die) {
         int tr, ts, range;
@@ -537,20 +553,26 @@ template <typename T, bool CHANNELS, bool SPLIT> __global__ void __launch_bounds
         float s = 0.f;
         auto step = [&](auto which, int k) {
             constexpr int KK = decltype(which)::value;
-            FC_ARRIVED(2 + 3);                                   // this step's pieces are there (of the two after it, three and two transfers); every wave has read the last one's
             const char *const here = lds + stage * STAGE, *const scales = own + stage * 256;
-            const int free_stage = stage == 0 ? STAGES - 1 : stage - 1;
+            const int next = stage + 1 < STAGES ? stage + 1 : 0;
+            if (ALONE && KK == 0) s = *(const float *)(scales + l32 * 4) * *(const float *)(scales + 128);
+            // This step's pieces (ALONE: the next one's) are there, those of the two after it on their way; every wave has read the last one's (this one's).
+            FC_ARRIVED(2 + 3);
             // (the tile's last one is asked for after its results, which go by way of that stage)
-            if (k + 1 < steps) fetch(free_stage);
-            if (KK == 0) s = *(const float *)(scales + l32 * 4) * *(const float *)(scales + 128);
-            const Half fs = {*(const uint4 *)(here + so), *(const uint4 *)(here + (so ^ 32))};
+            if (k + 1 < steps) fetch(ALONE ? stage : stage == 0 ? STAGES - 1 : stage - 1);
+            if (!ALONE && KK == 0) s = *(const float *)(scales + l32 * 4) * *(const float *)(scales + 128);
+            if constexpr (ALONE) {
+                read(KK ^ 1, lds + next * STAGE);
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
+                read(0, here);
+            }
 #pragma unroll
             for (int i = 0; i < FR; ++i) {
-                const Half fr = {*(const uint4 *)(here + ro + i * 2048), *(const uint4 *)(here + (ro ^ 32) + i * 2048)};
                 if (KK == 0) p[i] = f32x16{};
-                product_of<CLOSE>(fr, fs, p[i]);
+                product_of<CLOSE>(fr[ALONE ? KK : 0][i], fs[ALONE ? KK : 0], p[i]);
             }
-            stage = stage + 1 < STAGES ? stage + 1 : 0;
+            stage = next;
         };
         auto add = [&] {
 #pragma unroll
@@ -567,9 +589,9 @@ template <typename T, bool CHANNELS, bool SPLIT> __global__ void __launch_bounds
         if (k < steps) {                                         // (a last block of one step)
             step(std::integral_constant<int, 0>(), k);
             add();
+            if (ALONE) fr[0][0] = fr[1][0], fr[0][1] = fr[1][1], fs[0] = fs[1];
         }
-        const int free_stage = (stage + 2) & 3;                  // the last step's but one
-        static_assert(STAGES == 4, "stages in turn");
+        const int free_stage = (stage + (ALONE ? 3 : 2)) & 3;    // the last step's, or the one's before it: every wave has read it
         const int r1 = r0 + wr * FR * 32, s1 = s0 + wsv * 32;
         if constexpr (SPLIT) {
             float *const part = a.part + (int64_t)range * a.T * a.O;
@@ -596,8 +618,8 @@ template <typename T, bool CHANNELS, bool SPLIT> __global__ void __launch_bounds
         if constexpr (sizeof(T) == 2) {
             if (whole) {
                 done = true;
-                // The stage of the last step but one: every wave has read it, and what comes there next is, in a wave's own 2 KB, that wave's own transfers. The bias
-                // is there three steps after it was asked for; with fewer steps it is waited for.
+                // What comes to the free stage next is, in a wave's own 2 KB, that wave's own transfers. The bias is there three steps after it was asked for; with
+                // fewer steps it is waited for.
                 if (steps < 4) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 char *const mine = lds + free_stage * STAGE + wave * 2048;
                 const float *const bias = (const float *)(own + STAGES * 256);
@@ -654,7 +676,7 @@ template <typename T> __global__ void __launch_bounds__(256) k_f8_sums(const F8A
 static int f8_ranges(int64_t T, int64_t K, int64_t O)
 {
     const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128), blocks = (K + 127) / 128;
-    if (T <= 64 || K % 16 != 0 || tiles > 64) return 1;
+    if (T <= 64 || K % 16 != 0 || tiles >= 128) return 1;
     const int64_t most = 256 / tiles < blocks / 4 ? 256 / tiles : blocks / 4;
     if (most < 2) return 1;
     const int64_t per = (blocks + most - 1) / most;
@@ -755,7 +777,7 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
     a.ranges = f8_ranges(a.T, a.K, a.O);
     if (pieces && a.ranges > 1) {
         a.per = (a.blocks + a.ranges - 1) / a.ranges, a.part = (float *)workspace;
-        FC_TRY(launch_async(k_f8_small<T, false, true>, 128, SMALL_LDS, 512));
+        FC_TRY(launch_async(k_f8_small<T, false, true, true>, 128, SMALL_LDS, 256));
         k_f8_sums<T><<<(unsigned)(((int64_t)a.T * a.O + 1023) / 1024), 256, 0, s>>>(a);
         FC_HIP(hipGetLastError());
         return FFTCONV_OK;
@@ -764,7 +786,10 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
     if constexpr (sizeof(T) == 2) {
         if (pieces && tiles(256) >= 256) return a.channels ? launch_async(k_f8_large<T, true>, 256, LARGE_LDS, 256) : launch_async(k_f8_large<T, false>, 256, LARGE_LDS, 256);
     }
-    if (pieces && tiles(128) >= 128) return a.channels ? launch_async(k_f8_small<T, true, false>, 128, SMALL_LDS, 512) : launch_async(k_f8_small<T, false, false>, 128, SMALL_LDS, 512);
+    if (pieces && tiles(128) >= 128 && tiles(128) <= 256)            // (one to a compute unit)
+        return a.channels ? launch_async(k_f8_small<T, true, false, true>, 128, SMALL_LDS, 256) : launch_async(k_f8_small<T, false, false, true>, 128, SMALL_LDS, 256);
+    if (pieces && tiles(128) > 256)
+        return a.channels ? launch_async(k_f8_small<T, true, false, false>, 128, SMALL_LDS, 512) : launch_async(k_f8_small<T, false, false, false>, 128, SMALL_LDS, 512);
     if (tiles(128) >= 256) return launch(integral_constant<int, 2>());
     return launch(integral_constant<int, 1>());
 }
