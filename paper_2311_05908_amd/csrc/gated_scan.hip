@@ -9,7 +9,7 @@
 // exchanges inside the vector unit, the four rows of a wave one after the other with what comes in), and each walks its samples once more from
 // what the lanes before it leave. A wave takes 512 samples of a row at a time, eight in a run for each lane; short rows get part of a wave.
 // Everything between the load of u, w, v (and dy) and the store of y (du, dw, dv) is fp32 in registers: every tensor moves once, and that is what
-// bounds these kernels: bf16 64 x 768 x 4096 forward 296 us, 5.4 TB/s, backward 527 us, 5.3 TB/s. What comes next is asked for before the samples in
+// bounds these kernels: bf16 64 x 768 x 4096 forward 295 us, 5.5 TB/s, backward 510 us, 5.5 TB/s. What comes next is asked for before the samples in
 // hand are worked on: 1024 rows of 65536 164 and 202 us, without 261 and 364.
 //
 // Few rows: a row goes in segments to waves of their own. A first kernel composes each segment to one map, and every wave of the second applies
@@ -29,7 +29,7 @@ struct ScanArgs {
     float2 *maps;                 // (rows, segments): a segment as one map
     int64_t rows, N, first;       // first: row of a launch's first workgroup
     int C, chunks, segments, per; // pieces of 512 samples to a row; segments of a row, pieces of one
-    int log_gate;
+    int log_gate, beyond_cache;   // beyond_cache: a result is larger than the memory-side cache (256 MB)
 };
 
 constexpr int SE = 8;             // samples of a lane
@@ -57,6 +57,20 @@ template <typename T> __device__ __forceinline__ void gate_of(float w, bool log_
     const float t = exp_below_one<CLOSE>(-fabsf(w)), d = 1.f + t, r0 = __builtin_amdgcn_rcpf(d), r = fmaf(fmaf(-d, r0, 1.f), r0, r0), tr = t * r;
     a = w >= 0.f ? r : tr;
     rest = w >= 0.f ? tr : r;
+}
+
+// Eight results of a lane. Past the caches where a tensor is larger than the memory-side one and pushes everything else out of it: bf16 64 x 768 x 4096 305 -> 295 us,
+// with the gradients 840 -> 806. (fp32, whose eight are two stores of half a line, goes through them.)
+template <typename T> __device__ __forceinline__ void put(T *p, int64_t left, const T (&v)[SE], int beyond_cache)
+{
+    if (sizeof(T) == 2 && beyond_cache && left >= SE) {
+        typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4;
+        u32x4 w;
+        __builtin_memcpy(&w, v, sizeof(w));
+        __builtin_nontemporal_store(w, (u32x4 *)p);
+    } else {
+        store_piece<T, SE>(p, left, v);
+    }
 }
 
 template <int CTRL, bool ZERO> __device__ __forceinline__ float dpp_f32(float outside, float x)
@@ -249,7 +263,7 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
             }
         }
         if (there) {
-            if (!WHOLE || col < g.N) store_piece<T, SE>((T *)g.y + row * g.N + col, WHOLE ? SE : g.N - col, y);
+            if (!WHOLE || col < g.N) put<T>((T *)g.y + row * g.N + col, WHOLE ? SE : g.N - col, y, g.beyond_cache);
         }
     }
     if (g.last && lane == 0 && there && seg == g.segments - 1) g.last[row] = h;
@@ -307,7 +321,7 @@ template <typename T, bool BACK, bool WHOLE> __global__ void __launch_bounds__(2
     if (lane == 0) g.maps[row * g.segments + seg] = make_float2(m.a, m.x);
 }
 
-template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) k_scan_back(const ScanArgs g)
+template <typename T, int G, bool WHOLE, bool AHEAD> __global__ void __launch_bounds__(256) k_scan_back(const ScanArgs g)
 {
     const int lane = threadIdx.x & (G - 1);
     int64_t row = g.first + (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
@@ -339,8 +353,9 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
         kept = g.kept_in[row * g.chunks + k];
     };
     const int top = min((seg + 1) * g.per, g.chunks) - 1;
-    ask(top);
+    if (AHEAD) ask(top);
     for (int k = top; k >= first; --k) {
+        if (!AHEAD) ask(k);
         const int64_t begin = (int64_t)k * (G * SE), col = begin + lane * SE;
         T du[SE] = {}, dw[SE] = {}, dv[SE] = {};
         if (begin < len) {
@@ -349,7 +364,7 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
             q.take(g, ru, rw, col, len, all);
             const Raw<T> w = rw, dy = rdy, v = rv;
             float h = kept, d[SE];
-            ask(k - 1);
+            if (AHEAD) ask(k - 1);
             float s = into_lane<false, G>(q.map(), h);
             Map m = {1.f, 0.f};
 #pragma unroll
@@ -382,14 +397,14 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
                 dw[e] = from_f32<T>(in ? gw : 0.f);
                 dv[e] = from_f32<T>(in ? to_f32(dy.v[e]) * s : 0.f);
             }
-        } else {
+        } else if (AHEAD) {
             ask(k - 1);
         }
         if (there && (!WHOLE || col < g.N)) {
             const int64_t at = row * g.N + col, left = WHOLE ? SE : g.N - col;
-            store_piece<T, SE>((T *)g.du + at, left, du);
-            store_piece<T, SE>((T *)g.dw + at, left, dw);
-            if (g.v) store_piece<T, SE>((T *)g.dv + at, left, dv);
+            put<T>((T *)g.du + at, left, du, g.beyond_cache);
+            put<T>((T *)g.dw + at, left, dw, g.beyond_cache);
+            if (g.v) put<T>((T *)g.dv + at, left, dv, g.beyond_cache);
         }
     }
     if (g.dstate && lane == 0 && there && seg == 0) g.dstate[row] = p;
@@ -443,6 +458,7 @@ template <typename T> static int run(ScanArgs &g, bool back, hipStream_t s)
     const bool whole = g.N % SE == 0;
     g.chunks = (int)((g.N + lanes * SE - 1) / (lanes * SE));
     g.segments = scan_segments(g.rows, g.N);
+    g.beyond_cache = g.rows * g.N > ((int64_t)256 << 20) / (int64_t)sizeof(T);
     g.per = (g.chunks + g.segments - 1) / g.segments;
     auto launch = [&](auto kernel, int64_t groups) -> int {
         return in_pieces(groups, 256, [&](int64_t first, unsigned n) -> int {
@@ -459,10 +475,12 @@ template <typename T> static int run(ScanArgs &g, bool back, hipStream_t s)
     }
     const int64_t groups = (g.rows * g.segments + 256 / lanes - 1) / (256 / lanes);
     if (back) {
-        if (lanes == 1) return launch(k_scan_back<T, 1, false>, groups);
-        if (lanes == 4) return launch(k_scan_back<T, 4, false>, groups);
-        if (lanes == 16) return launch(k_scan_back<T, 16, false>, groups);
-        return launch(whole ? k_scan_back<T, 64, true> : k_scan_back<T, 64, false>, groups);
+        if (lanes == 1) return launch(k_scan_back<T, 1, false, false>, groups);
+        if (lanes == 4) return launch(k_scan_back<T, 4, false, false>, groups);
+        if (lanes == 16) return launch(k_scan_back<T, 16, false, false>, groups);
+        // (with 64 waves to a compute unit enough is on its way without asking ahead: bf16 64 x 768 x 4096 forward and backward 806 us, with it 818)
+        if (g.rows * g.segments >= 16384) return launch(whole ? k_scan_back<T, 64, true, false> : k_scan_back<T, 64, false, false>, groups);
+        return launch(whole ? k_scan_back<T, 64, true, true> : k_scan_back<T, 64, false, true>, groups);
     }
     if (lanes == 1) return launch(k_scan<T, 1, false>, groups);
     if (lanes == 4) return launch(k_scan<T, 4, false>, groups);

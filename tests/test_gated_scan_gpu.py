@@ -143,7 +143,7 @@ def test_scan_and_its_gradients(b, c, n, dtype, kind):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
-@pytest.mark.parametrize("b,c,n", [(64, 65, 600), (8, 1001, 516), (9, 700, 65), (40, 300, 5)])
+@pytest.mark.parametrize("b,c,n", [(64, 65, 600), (8, 1001, 516), (9, 700, 65), (40, 300, 5), (64, 257, 520), (65, 256, 603)])
 def test_many_rows(b, c, n, dtype):
     """Rows that go to a wave or less each, and whose last wave is not full."""
     check(*make(b, c, n, dtype, "sigmoid", True, True, True), "sigmoid", dtype)
