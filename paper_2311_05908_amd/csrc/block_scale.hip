@@ -3,7 +3,8 @@
 //   s = max |x| / 448 over the block,  q = x / s rounded to e4m3, to nearest even
 //
 // A block stays in registers from its load to its store, so the bytes bound these kernels; what is turned over on the way (rows from tensors that
-// lie channel by channel, a weight's transpose) goes through LDS as bytes.
+// lie channel by channel, a weight's transpose) goes through LDS as bytes. Measured: fp32 16384 x 4096 with its transpose 82 us, 4.9 TB/s; bf16 3 x 64 x 768
+// x 4096 to rows of 2304 340 us, 5.4 TB/s; f16 8192 x 4096 25 us, 4 TB/s; one row 3.4 us, of which the launch is most.
 #include "layers_index.h"
 #include "layers_internal.h"
 

@@ -200,18 +200,35 @@ __device__ __forceinline__ int64_t length_of(const ScanArgs &g, int64_t row)
     return n < 0 ? 0 : n < g.N ? n : g.N;
 }
 
-// Maps of a row's segments from `begin` on, `count` of them, applied to `in` one after the other (REVERSE: from the last).
-template <bool REVERSE> __device__ __forceinline__ float through_segments(const float2 *maps, int begin, int count, float in)
-{
-    const int lane = threadIdx.x & 63;
-    for (int i = 0; i < count; i += 64) {
-        const int k = REVERSE ? count - 1 - (i + 63 - lane) : i + lane;          // (the lanes' order is the samples')
-        Map m = {1.f, 0.f};
-        if (k >= 0 && k < count) m = {maps[begin + k].x, maps[begin + k].y};
-        into_lane<REVERSE, 64>(m, in);
+// Maps of `count` of a row's segments, applied to `in` one after the other (REVERSE: from the last): 256 at a time, four in a run for each lane. The first
+// 256 are asked for when this is made, so that what else a wave reads is on its way behind them.
+template <bool REVERSE> struct Segments {
+    const float2 *maps;
+    int count;
+    float2 m[4];
+    __device__ __forceinline__ void load(int base)
+    {
+        const int k0 = (REVERSE ? count - base - 256 : base) + (int)(threadIdx.x & 63) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = k0 + e >= 0 && k0 + e < count ? maps[k0 + e] : make_float2(1.f, 0.f);
     }
-    return in;
-}
+    __device__ __forceinline__ Segments(const float2 *maps, int count) : maps(maps), count(count) { load(0); }
+    __device__ __forceinline__ float through(float in)
+    {
+        for (int base = 0; base < count; base += 256) {
+            if (base > 0) load(base);
+            Map one = {1.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = REVERSE ? 3 - i : i;
+                one.x = fmaf(m[e].x, one.x, m[e].y);
+                one.a *= m[e].x;
+            }
+            into_lane<REVERSE, 64>(one, in);
+        }
+        return in;
+    }
+};
 
 // A workgroup's rows: 256 / G of them, or with G = 64 segments of rows, four of them.
 template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) k_scan(const ScanArgs g)
@@ -231,10 +248,6 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
     const bool there = row < g.rows;                             // (lanes exchange what they hold: none leaves a wave early)
     row = there ? row : g.rows - 1;
     const int64_t len = length_of(g, row);
-    float h = g.state ? g.state[row] : 0.f;
-    if constexpr (G == 64) {
-        if (seg > 0) h = through_segments<false>(g.maps + row * g.segments, 0, seg, h);
-    }
     const int end = min((seg + 1) * g.per, g.chunks);
     Raw<T> u, w, v;
     auto ask = [&](int k) {
@@ -244,7 +257,10 @@ template <typename T, int G, bool WHOLE> __global__ void __launch_bounds__(256) 
         w.template load<WHOLE>(g.w, row, col, g.N);
         if (g.v) v.template load<WHOLE>(g.v, row, col, g.N);
     };
+    float h = g.state ? g.state[row] : 0.f;
+    Segments<false> before(g.maps + row * g.segments, G == 64 ? seg : 0);
     ask(seg * g.per);
+    h = before.through(h);
     for (int k = seg * g.per; k < end; ++k) {
         const int64_t begin = (int64_t)k * (G * SE), col = begin + lane * SE;
         if (g.kept && lane == 0 && there) g.kept[row * g.chunks + k] = h;
@@ -336,10 +352,6 @@ template <typename T, int G, bool WHOLE, bool AHEAD> __global__ void __launch_bo
     const bool there = row < g.rows;
     row = there ? row : g.rows - 1;
     const int64_t len = length_of(g, row);
-    float p = g.dlast ? g.dlast[row] : 0.f;
-    if constexpr (G == 64) {
-        if (seg < g.segments - 1) p = through_segments<true>(g.maps + row * g.segments, seg + 1, g.segments - 1 - seg, p);
-    }
     const int first = seg * g.per;
     Raw<T> ru, rw, rv, rdy;
     float kept = 0.f;
@@ -353,9 +365,11 @@ template <typename T, int G, bool WHOLE, bool AHEAD> __global__ void __launch_bo
         kept = g.kept_in[row * g.chunks + k];
     };
     const int top = min((seg + 1) * g.per, g.chunks) - 1;
-    if (AHEAD) ask(top);
+    float p = g.dlast ? g.dlast[row] : 0.f;
+    Segments<true> behind(g.maps + row * g.segments + seg + 1, G == 64 ? g.segments - 1 - seg : 0);
+    ask(top);
+    p = behind.through(p);
     for (int k = top; k >= first; --k) {
-        if (!AHEAD) ask(k);
         const int64_t begin = (int64_t)k * (G * SE), col = begin + lane * SE;
         T du[SE] = {}, dw[SE] = {}, dv[SE] = {};
         if (begin < len) {
@@ -406,6 +420,7 @@ template <typename T, int G, bool WHOLE, bool AHEAD> __global__ void __launch_bo
             put<T>((T *)g.dw + at, left, dw, g.beyond_cache);
             if (g.v) put<T>((T *)g.dv + at, left, dv, g.beyond_cache);
         }
+        if (!AHEAD) ask(k - 1);
     }
     if (g.dstate && lane == 0 && there && seg == 0) g.dstate[row] = p;
 }
@@ -478,8 +493,9 @@ template <typename T> static int run(ScanArgs &g, bool back, hipStream_t s)
         if (lanes == 1) return launch(k_scan_back<T, 1, false, false>, groups);
         if (lanes == 4) return launch(k_scan_back<T, 4, false, false>, groups);
         if (lanes == 16) return launch(k_scan_back<T, 16, false, false>, groups);
-        // (with 64 waves to a compute unit enough is on its way without asking ahead: bf16 64 x 768 x 4096 forward and backward 806 us, with it 818)
-        if (g.rows * g.segments >= 16384) return launch(whole ? k_scan_back<T, 64, true, false> : k_scan_back<T, 64, false, false>, groups);
+        // With 64 waves to a compute unit enough is on its way without asking ahead (bf16 64 x 768 x 4096 forward and backward 806 us, with it 818), and waves of
+        // one piece have nothing to ask for: without, four of fp32 fit where three do with it (1 x 16 x 131072 12.5 us).
+        if (g.per == 1 || g.rows * g.segments >= 16384) return launch(whole ? k_scan_back<T, 64, true, false> : k_scan_back<T, 64, false, false>, groups);
         return launch(whole ? k_scan_back<T, 64, true, true> : k_scan_back<T, 64, false, true>, groups);
     }
     if (lanes == 1) return launch(k_scan<T, 1, false>, groups);

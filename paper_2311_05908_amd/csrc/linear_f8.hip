@@ -684,7 +684,8 @@ static int f8_ranges(int64_t T, int64_t K, int64_t O)
 }
 
 // Few tokens (up to 16 NT): what counts is how fast the weight streams in, so its rows go from memory straight into the operand registers, sixteen
-// rows to a workgroup, whose waves divide the blocks of k among themselves and add their sums up in LDS.
+// rows to a workgroup, whose waves divide the blocks of k among themselves and add their sums up in LDS. Measured: 1 x 4096 -> 4096 5.3 us, 3.2 TB/s of the
+// weight's 16.8 MB, of which a launch is about half.
 template <typename T, int NT> __global__ void __launch_bounds__(512) k_f8_few(const F8Args a)
 {
     __shared__ f32x4 sums[8][NT][64];

@@ -1,9 +1,10 @@
-"""What stands around a long convolution in a layer: norm, 8-bit projections, activations kept in 8 bits (see include/fftconv.h, "The layers
-around a convolution").
+"""What stands around a long convolution in a layer: norm, 8-bit projections, activations kept in 8 bits; a gated recurrence for its place; clipping of
+gradients (see include/fftconv.h, from "The layers around a convolution" on).
 
     rows, h, rstd = layers.rms_norm_i8(x, weight, residual=r)                  # (b, n, d): h = x + r, its norm in 8 bits
     u, w, v = layers.linear_i8(rows, in_proj, layout="channels", parts=3)      # three of (b, h, n), what Plan.forward_gated takes
     y = plan.forward_gated(u, w, v, kf)
+    y, state = layers.gated_scan(u, w, v=v)                                    # or a recurrence, and its state
 
 Argument marshalling only, as in fftconv.py: every step runs in the HIP kernels of the library, on the current stream of the current
 device; PyTorch supplies memory. Tensors that are not laid out as a call wants them are refused, not copied.

@@ -43,7 +43,25 @@ def walk(a, x, k, start):
     return out
 
 
-def reference(u, w, v, state, lengths, kind, dy=None, dlast=None):
+def walk_far(a, x, k, start):
+    """The same for long rows, on the GPU: steps of 1, 2, 4, ... samples composed, in 64 bits."""
+    a, x, k, start = (torch.from_numpy(np.ascontiguousarray(t)).cuda() for t in (a, x, k, start))
+
+    def composed(x, first):
+        g, x = a.clone(), torch.cat([x[..., :1] + a[..., :1] * first[..., None], x[..., 1:]], -1)
+        shift = 1
+        while shift < a.shape[-1]:
+            x = torch.cat([x[..., :shift], x[..., shift:] + g[..., shift:] * x[..., :-shift]], -1)
+            g = torch.cat([g[..., :shift], g[..., shift:] * g[..., :-shift]], -1)
+            shift *= 2
+        return x
+
+    h, m = composed(x, start), composed(x.abs(), start.abs())
+    e = composed((k + 2) * E * (a * torch.cat([start.abs()[..., None], m[..., :-1]], -1) + x.abs()), torch.zeros_like(start))
+    return torch.stack([h, e + 32 * E * m, m]).cpu().numpy()
+
+
+def reference(u, w, v, state, lengths, kind, dy=None, dlast=None, walk=walk):
     """name -> (value, bound before the rounding to the result's type)"""
     u, w, v, state, dy, dlast = (data(t) for t in (u, w, v, state, dy, dlast))
     b, c, n = u.shape
@@ -113,8 +131,8 @@ def make(b, c, n, dtype, kind, gated, state, ragged, seed=0, offset=0):
         dy=normal(b, c, n), dlast=normal(b, c, to=f32) if state else None)
 
 
-def check(fwd, bwd, kind, dtype):
-    ref = reference(**fwd, kind=kind, **bwd)
+def check(fwd, bwd, kind, dtype, walk=walk):
+    ref = reference(**fwd, kind=kind, **bwd, walk=walk)
     y, last, kept = layers.gated_scan(**fwd, gate=kind, keep=True)
     y2, last2 = layers.gated_scan(**fwd, gate=kind)
     assert torch.equal(y, y2) and torch.equal(last, last2)
@@ -147,6 +165,13 @@ def test_scan_and_its_gradients(b, c, n, dtype, kind):
 def test_many_rows(b, c, n, dtype):
     """Rows that go to a wave or less each, and whose last wave is not full."""
     check(*make(b, c, n, dtype, "sigmoid", True, True, True), "sigmoid", dtype)
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "log"])
+@pytest.mark.parametrize("b,c,n,dtype", [(1, 2, 140001, "f32"), (2, 1, 262144, "bf16"), (1, 1, 600000, "f16"), (1, 300, 9001, "f32"), (3, 350, 5000, "bf16")])
+def test_long_rows(b, c, n, dtype, kind):
+    """Rows of more segments than a wave takes at a time, and rows about the lines between one segment and several."""
+    check(*make(b, c, n, dtype, kind, True, True, b > 1), kind, dtype, walk=walk_far)
 
 
 @pytest.mark.parametrize("dtype", list(DT))
