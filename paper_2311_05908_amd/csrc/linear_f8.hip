@@ -293,11 +293,11 @@ template <typename T, bool CHANNELS> __global__ void __launch_bounds__(512, 2) k
         int tr, ts;
         walk.place(min(f_tile, last - 1), tr, ts, a.tiles_r);
         const int row0 = (is_r ? tr : ts) * block;
-        base = (const char *)(is_r ? a.w : a.x) + (int64_t)row0 * a.K - 3072;
+        base = (const char *)(is_r ? a.w : a.x) + (int64_t)row0 * a.K - 3 * 1024;
 #pragma unroll
         for (int i = 0; i < LI; ++i) {
             const int row = (wave & 3) * 8 * LI + i * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
-            off[i] = (uint32_t)(min(row0 + row, rows - 1) - row0) * (uint32_t)a.K + piece * 16 + 3072 - (i % 4) * 1024;
+            off[i] = (uint32_t)(min(row0 + row, rows - 1) - row0) * (uint32_t)a.K + piece * 16 + 3 * 1024 - (i % 4) * 1024;
         }
         const int s0 = ts * BS;
         xs = (const char *)(a.xs + s0);
