@@ -256,6 +256,8 @@ int fftconv_gated_step(const void *u, const void *w, const void *v, const float 
     const int64_t to = size_of(dtype);
     if (!aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(y, to) || !aligned(state, 4) || !aligned(next, 4))
         return bad(who, "a tensor is not aligned to its elements");
+    if (next != state && (uintptr_t)next < (uintptr_t)(state + T) && (uintptr_t)state < (uintptr_t)(next + T))
+        return bad(who, "next overlaps state without being it");
     return lay::gated_step(u, w, v, state, next, y, T, gate, dtype, (hipStream_t)stream);
 }
 

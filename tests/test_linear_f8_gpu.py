@@ -199,6 +199,30 @@ def test_linear(b, n, k, o, dtype):
     within(layers.linear_f8(rows, weight, dtype=DT[dtype], layout="channels", parts=parts), laid(value, parts), laid(bound, parts), dtype)
 
 
+# Both tiles, a compute unit to a tile and two tiles to one, ranges of k, with one step of k, with odd numbers of them, with ends inside a piece of 128.
+STEPS = [(2048, 4096, 1), (2048, 8192, 0), (8192, 4096, 0), (2048, 2560, 0), (1500, 1500, 0), (1408, 1408, 1), (4100, 4350, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k", [16, 64, 80, 128, 144, 192, 320, 336])
+@pytest.mark.parametrize("t,o,with_bias", STEPS)
+def test_few_steps_of_k(t, o, k, with_bias, dtype):
+    rows, weight, bias = operands(gen(k + o + t), 1, t, k, o, bias=bool(with_bias))
+    value, bound = product(rows, weight, bias)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype]), value, bound, dtype)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("t,k,o", [(300, 1104, 512), (300, 1056, 512), (100, 1040, 130), (65, 16384, 100), (1, 1 << 20, 40), (40, (1 << 18) + 16, 33), (70, (1 << 18) + 80, 130),
+                                   (66, 4097, 70), (600, 3000, 1700), (128, 2176, 4096)])
+def test_ranges_and_long_rows(t, k, o, dtype):
+    rows, weight, bias = operands(gen(k + o + t), 1, t, k, o)
+    value, bound = product(rows, weight, bias)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype]), value, bound, dtype)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
+
+
 def test_sums_are_as_fine_as_fp32():
     """Blocks whose products cancel but for one: 448^2 = 49 2^12 and 2^-2 add up within fp32's 24 bits, so what remains is exact, where
     products that keep 13 bits below the largest leave nothing."""

@@ -124,3 +124,32 @@ def test_a_step_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(y, want[t][0]) and torch.equal(s, want[t][1])
         layer.step(x[0], r[0], torch.zeros_like(s))
+
+
+def test_two_streams_at_once():
+    """Calls with workspaces of their own on two streams, over and over: what one stream alone gives."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=g, device="cuda").to(torch.bfloat16)
+
+    def work(x, weight, u, w, v, dy, grads):
+        y = layers.linear_f8(layers.quantize_blocks(x), weight)
+        h, last, kept = layers.gated_scan(u, w, v=v, keep=True)
+        d, dstate = layers.gated_scan_backward(dy, u, w, kept, v=v)
+        out = [torch.empty_like(t) for t in grads]
+        return [y, h, last, d, dstate, layers.clip_grads(grads, 1.0, out=out), *out]
+
+    inputs = [(normal(100, 4096), layers.quantize_tiles(normal(512, 4096)), *(normal(2, 20, 9000) for _ in range(4)), [normal(5000), normal(70, 33)]) for _ in range(2)]
+    want = [work(*i) for i in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(20):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(work(*inputs[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for one in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(one, want[k]))

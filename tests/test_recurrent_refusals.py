@@ -50,7 +50,7 @@ def test_step():
     def step(u=A, w=A, v=None, state=A, to=A, y=A, t=5, gate=0, dtype=F32):
         return call("fftconv_gated_step", u, w, v, state, to, y, t, gate, dtype, None)
     for kw in (dict(u=None), dict(w=None), dict(state=None), dict(to=None), dict(y=None), dict(t=-1), dict(t=1 << 31), dict(gate=3), dict(dtype=5), dict(u=A + 2),
-               dict(state=A + 1), dict(to=A + 2), dict(v=A + 2)):
+               dict(state=A + 1), dict(to=A + 2), dict(v=A + 2), dict(to=A + 4), dict(to=A - 16)):
         assert step(**kw) == EINVAL, kw
     assert step(t=0, u=None, w=None, state=None, to=None, y=None) == OK
 
