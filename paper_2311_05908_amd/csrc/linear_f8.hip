@@ -7,9 +7,10 @@
 // number a lane, and the weight's scale is the same in the whole wave. Token by token a lane's four consecutive rows are neighbours in y; channel by
 // channel the lanes are.
 //
-// Which kernel: up to 64 tokens k_f8_few, bound by the weight's bytes. Above, with k in pieces of 16 bytes (both operands aligned to them),
-// k_f8_async: on tiles of 256 x 256 where there is one for every compute unit, else on 128 x 128 where there are 128 of those, and with k in ranges
-// where there are 64 or less and k is 2048 or more. Everything else is k_f8's, which takes any k at any alignment.
+// Which kernel: up to 64 tokens k_f8_few, bound by the weight's bytes. Above, with k in pieces of 16 bytes (both operands aligned to them), k_f8_large on
+// tiles of 256 x 256 where there is one for every compute unit, else k_f8_small on 128 x 128 where there are 128 of those, or with k in ranges where there
+// are fewer and k is 1024 or more. Rows of other lengths are laid out again for these where that pays (f8_padded); everything else is k_f8's, which
+// takes any k at any alignment.
 #include "layers_index.h"
 #include "linear_common.h"
 
@@ -672,11 +673,35 @@ template <typename T> __global__ void __launch_bounds__(256) k_f8_sums(const F8A
     }
 }
 
+// Rows whose length is no multiple of 16 are laid out again at a distance that is one, with zeros behind them, tokens and weight one after the other, where
+// the products are worth the bytes and another launch. In us, as they are and so: 4095 -> 4096 64 tokens 44 and 23, 300 67 and 33, 8192 386 and 161; 8191 -> 1000
+// 100 tokens 60 and 24, 64 tokens 78 either way; 2047 -> 4096 100 tokens 29 and 23; but 1001 -> 3001 300 tokens 14 and 20, 512 16 and 24, 2048 34 and 26.
+static bool f8_padded(int64_t T, int64_t K, int64_t O)
+{
+    return T > 16 && K % 16 != 0 && (double)T * (double)O * (double)K >= (double)((int64_t)1 << (K >= 2000 ? 29 : 32));
+}
+struct PadArgs {
+    const uint8_t *x, *w;
+    uint8_t *to;
+    int64_t T, K, first, pitch;   // first: row of a launch's first piece
+    int pieces, count;            // of 16 bytes: of a row, of the launch
+    uint32_t by_pieces;
+};
+__global__ void __launch_bounds__(256) k_f8_pad(const PadArgs a)
+{
+    const int i = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (i >= a.count) return;
+    const int r = quotient(i, a.pieces, a.by_pieces), p = i - r * a.pieces;
+    const int64_t row = a.first + r;
+    const uint4 v = load16(row < a.T ? a.x + row * a.K : a.w + (row - a.T) * a.K, (int64_t)p * 16, a.K);
+    *(uint4 *)(a.to + row * a.pitch + p * 16) = v;
+}
+
 // Into how many ranges k goes: where few tiles are left for the compute units, as many as give each one, of four blocks at least.
 static int f8_ranges(int64_t T, int64_t K, int64_t O)
 {
     const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128), blocks = (K + 127) / 128;
-    if (T <= 64 || K % 16 != 0 || tiles >= 128) return 1;
+    if (T <= 64 || (K % 16 != 0 && !f8_padded(T, K, O)) || tiles >= 128) return 1;
     const int64_t most = 256 / tiles < blocks / 4 ? 256 / tiles : blocks / 4;
     if (most < 2) return 1;
     const int64_t per = (blocks + most - 1) / most;
@@ -742,6 +767,21 @@ template <typename T, int NT> __global__ void __launch_bounds__(512) k_f8_few(co
 
 template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
 {
+    bool pieces = a.K % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.w) % 16 == 0;
+    a.ranges = f8_ranges(a.T, a.K, a.O);
+    if (f8_padded(a.T, a.K, a.O)) {
+        const int64_t rows = (int64_t)a.T + a.O;
+        PadArgs p = {a.x, a.w, (uint8_t *)(((uintptr_t)workspace + 15) & ~(uintptr_t)15), a.T, a.K, 0, (a.K + 15) / 16 * 16, (int)((a.K + 15) / 16), 0, 0};
+        p.by_pieces = reciprocal(p.pieces);
+        const int64_t most = ((int64_t)1 << 30) / p.pieces;      // rows to a launch, whose pieces are a number of 32 bits
+        for (; p.first < rows; p.first += most) {
+            p.count = (int)((rows - p.first < most ? rows - p.first : most) * p.pieces);
+            k_f8_pad<<<(unsigned)((p.count + 255) / 256), 256, 0, s>>>(p);
+            FC_HIP(hipGetLastError());
+        }
+        a.x = p.to, a.w = p.to + a.T * p.pitch, a.K = p.pitch, pieces = true;
+        workspace = p.to + rows * p.pitch;
+    }
     if (a.T <= 64) {
         return in_pieces(((int64_t)a.O + 15) / 16, 512, [&](int64_t first, unsigned g) -> int {
             a.first = (int)first;
@@ -773,9 +813,7 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
     };
     constexpr int LARGE_LDS = 2 * 512 * 128 + 8 * (2 * 512 + 512), SMALL_LDS = 4 * 256 * 64 + 8 * (4 * 256 + 256);
     auto tiles = [&](int64_t b) { return ((a.O + b - 1) / b) * ((a.T + b - 1) / b); };
-    const bool pieces = a.K % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.w) % 16 == 0;
     using std::integral_constant;
-    a.ranges = f8_ranges(a.T, a.K, a.O);
     if (pieces && a.ranges > 1) {
         a.per = (a.blocks + a.ranges - 1) / a.ranges, a.part = (float *)workspace;
         FC_TRY(launch_async(k_f8_small<T, false, true, true>, 128, SMALL_LDS, 256));
@@ -798,7 +836,7 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
 size_t linear_f8_workspace(int64_t T, int64_t K, int64_t O)
 {
     const int ranges = f8_ranges(T, K, O);
-    return ranges > 1 ? (size_t)ranges * (size_t)T * (size_t)O * 4 : 0;
+    return (ranges > 1 ? (size_t)ranges * (size_t)T * (size_t)O * 4 : 0) + (f8_padded(T, K, O) ? (size_t)(T + O) * (size_t)((K + 15) / 16 * 16) + 16 : 0);
 }
 
 int linear_f8(const uint8_t *x, const float *xs, const uint8_t *w, const float *ws, const float *bias, void *y, int64_t B, int64_t N, int64_t K,

@@ -215,7 +215,8 @@ def test_few_steps_of_k(t, o, k, with_bias, dtype):
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("t,k,o", [(300, 1104, 512), (300, 1056, 512), (100, 1040, 130), (65, 16384, 100), (1, 1 << 20, 40), (40, (1 << 18) + 16, 33), (70, (1 << 18) + 80, 130),
-                                   (66, 4097, 70), (600, 3000, 1700), (128, 2176, 4096)])
+                                   (66, 4097, 70), (600, 3000, 1700), (128, 2176, 4096), (40, 4095, 4096),
+                                   (300, 4001, 2100), (100, 2047, 4096), (4096, 2001, 4100), (3000, 1001, 2000)])
 def test_ranges_and_long_rows(t, k, o, dtype):
     rows, weight, bias = operands(gen(k + o + t), 1, t, k, o)
     value, bound = product(rows, weight, bias)
