@@ -8,7 +8,7 @@
 // channel the lanes are.
 //
 // Which kernel: up to 64 tokens k_f8_few, bound by the weight's bytes. Above, with k in pieces of 16 bytes (both operands aligned to them), k_f8_large on
-// tiles of 256 x 256 where there is one for every compute unit, else k_f8_small on 128 x 128 where there are 128 of those, or with k in ranges where there
+// tiles of 256 x 256 where these fill the compute units, else k_f8_small on 128 x 128 where there are 128 of those, or with k in ranges where there
 // are fewer and k is 1024 or more. Rows of other lengths are laid out again for these where that pays (f8_padded); everything else is k_f8's, which
 // takes any k at any alignment.
 #include "layers_index.h"
@@ -822,8 +822,13 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
         return FFTCONV_OK;
     }
     a.ranges = 1;
+    // The large tile where there is one for every compute unit, k has four blocks or more, and its last round of tiles leaves few units without one: a round of
+    // 256 takes as long as 1.55 to 2 rounds of 512 small ones, two of which share a unit. In us, large and small: 64 x 4096 x 768 -> 2304 (36 rounds) 686 and
+    // 855, 16384 x 768 -> 2304 (576 tiles) 62 and 53, 8192 x 768 -> 2304 (288) 42 and 31, 6400 x 1024 -> 7168 (700) 79 and 72, 65536 x 4096 -> 1024 (1024) 302 and
+    // 393; 65536 -> 4096 with k of 512 268 and 280, of 256 224 and 190.
     if constexpr (sizeof(T) == 2) {
-        if (pieces && tiles(256) >= 256) return a.channels ? launch_async(k_f8_large<T, true>, 256, LARGE_LDS, 256) : launch_async(k_f8_large<T, false>, 256, LARGE_LDS, 256);
+        if (pieces && a.blocks >= 4 && tiles(256) >= 256 && (double)tiles(128) / 512 > 1.85 * (double)((tiles(256) + 255) / 256))
+            return a.channels ? launch_async(k_f8_large<T, true>, 256, LARGE_LDS, 256) : launch_async(k_f8_large<T, false>, 256, LARGE_LDS, 256);
     }
     if (pieces && tiles(128) >= 128 && tiles(128) <= 256)            // (one to a compute unit)
         return a.channels ? launch_async(k_f8_small<T, true, false, true>, 128, SMALL_LDS, 256) : launch_async(k_f8_small<T, false, false, true>, 128, SMALL_LDS, 256);

@@ -213,6 +213,17 @@ def test_few_steps_of_k(t, o, k, with_bias, dtype):
     within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("b,n,k,o,parts", [(8, 1024, 512, 4096, 2), (1, 8190, 528, 4093, 1), (2, 4095, 1040, 4096, 4), (1, 8192, 640, 4092, 3), (32, 256, 768, 4096, 16),
+                                           (3, 2730, 400, 4100, 5)])
+def test_large_tiles(b, n, k, o, parts, dtype):
+    """Two tiles and more to a workgroup, inside the result and over its ends, over sequences' ends and parts'."""
+    rows, weight, bias = operands(gen(k + o + n), b, n, k, o)
+    value, bound = product(rows, weight, bias)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype]), value, bound, dtype)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels", parts=parts), laid(value, parts), laid(bound, parts), dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("t,k,o", [(300, 1104, 512), (300, 1056, 512), (100, 1040, 130), (65, 16384, 100), (1, 1 << 20, 40), (40, (1 << 18) + 16, 33), (70, (1 << 18) + 80, 130),
                                    (66, 4097, 70), (600, 3000, 1700), (128, 2176, 4096), (40, 4095, 4096),
