@@ -538,7 +538,7 @@ template <typename T, bool CHANNELS, bool SPLIT, bool ALONE> __global__ void __l
         for (int i = 0; i < FR; ++i) fr[buf][i] = {*(const uint4 *)(here + ro + i * 2048), *(const uint4 *)(here + (ro ^ 32) + i * 2048)};
         fs[buf] = {*(const uint4 *)(here + so), *(const uint4 *)(here + (so ^ 32))};
     };
-    if constexpr (ALONE) {
+    if constexpr (ALONE) {                                       // (or a step's are read when it comes)
         FC_ARRIVED(2 + 3 + 2);                                   // three transfers with a block's first step, two with its second
         read(0, lds);
     }
@@ -565,13 +565,19 @@ template <typename T, bool CHANNELS, bool SPLIT, bool ALONE> __global__ void __l
             if constexpr (ALONE) {
                 read(KK ^ 1, lds + next * STAGE);
                 __builtin_amdgcn_sched_barrier(0);
-            } else {
-                read(0, here);
-            }
 #pragma unroll
-            for (int i = 0; i < FR; ++i) {
-                if (KK == 0) p[i] = f32x16{};
-                product_of<CLOSE>(fr[ALONE ? KK : 0][i], fs[ALONE ? KK : 0], p[i]);
+                for (int i = 0; i < FR; ++i) {
+                    if (KK == 0) p[i] = f32x16{};
+                    product_of<CLOSE>(fr[KK][i], fs[KK], p[i]);
+                }
+            } else {
+                const Half tokens = {*(const uint4 *)(here + so), *(const uint4 *)(here + (so ^ 32))};
+#pragma unroll
+                for (int i = 0; i < FR; ++i) {
+                    const Half outputs = {*(const uint4 *)(here + ro + i * 2048), *(const uint4 *)(here + (ro ^ 32) + i * 2048)};
+                    if (KK == 0) p[i] = f32x16{};
+                    product_of<CLOSE>(outputs, tokens, p[i]);
+                }
             }
             stage = next;
         };
