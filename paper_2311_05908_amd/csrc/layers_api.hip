@@ -270,7 +270,7 @@ int fftconv_quantize_blocks(const void *x, int64_t ldx, uint8_t *q, float *scale
         set_error("%s: rows of K=%lld: up to %lld are supported", who, (long long)K, (long long)MOST_K_F8);
         return FFTCONV_EUNSUPPORTED;
     }
-    if (ldx < K || ldx > INT64_MAX / 64 / MOST) return bad(who, "the distance of rows is below K, or too large");
+    if (ldx < K || times(T, ldx, INT64_MAX / 64) < 0) return bad(who, "the distance of rows is below K, or too large");
     if (T == 0) return FFTCONV_OK;
     if (!x || !q || !scale) return bad(who, "a tensor is NULL");
     if (!aligned(x, size_of(dtype)) || !aligned(scale, 4)) return bad(who, "a tensor is not aligned to its elements");

@@ -276,7 +276,8 @@ template <typename T, bool CHANNELS> __global__ void __launch_bounds__(512, 2) k
     const int wr = wave >> 2, wsv = wave & 3;
     // tiles first, first + stride, ... below last
     const int wgs = gridDim.x, die = blockIdx.x % 8, dies = min(8, wgs), on_die = (wgs - die + 7) / 8;
-    const int begin = (int)((int64_t)walk.tiles * die / dies), last = (int)((int64_t)walk.tiles * (die + 1) / dies);
+    // (the dies that have a workgroup more have a tile more: 162 tiles, 1100 x 768 -> 2304, 11 us instead of 16)
+    const int begin = die * (walk.tiles / dies) + min(die, walk.tiles % dies), last = begin + walk.tiles / dies + (die < walk.tiles % dies ? 1 : 0);
     const int first = begin + blockIdx.x / 8;
     const bool tail = a.K % 128 != 0;
 
@@ -469,7 +470,8 @@ template <typename T, bool CHANNELS, bool SPLIT, bool ALONE> __global__ void __l
     const int wr = wave >> 2, wsv = wave & 3;
     // tiles first, first + stride, ... below last
     const int wgs = gridDim.x, die = blockIdx.x % 8, dies = min(8, wgs), on_die = (wgs - die + 7) / 8;
-    const int begin = (int)((int64_t)walk.tiles * die / dies), last = (int)((int64_t)walk.tiles * (die + 1) / dies);
+    // (the dies that have a workgroup more have a tile more: 162 tiles, 1100 x 768 -> 2304, 11 us instead of 16)
+    const int begin = die * (walk.tiles / dies) + min(die, walk.tiles % dies), last = begin + walk.tiles / dies + (die < walk.tiles % dies ? 1 : 0);
     const int first = begin + blockIdx.x / 8;
     const int all_steps = (int)((a.K + BK - 1) / BK);
     const bool tail = a.K % BK != 0;

@@ -79,6 +79,13 @@ def test_blocks_of_rows(t, k, dtype):
     same(layers.quantize_blocks(wide[:, 3:k + 3]), blocks8(wide[:, 3:k + 3]))
 
 
+def test_last_tokens_of_long_sequences():
+    """Rows at a distance of 10^8 values."""
+    x = torch.zeros(3, 131072, 768, dtype=torch.bfloat16, device="cuda")
+    x[:, -1] = normal(gen(8), 3, 768)
+    same(layers.quantize_blocks(x[:, -1]), blocks8(x[:, -1].contiguous()))
+
+
 def test_quotients_next_to_ties():
     """Values whose quotient is at the middle between two numbers of e4m3, or the fp32 numbers on either side, for many scales."""
     g = gen(1)

@@ -73,7 +73,7 @@ def test_linear(kw, rc):
 def test_quantisers():
     def rows(x=A, ld=64, q=A, s=A, t=2, k=64, dtype=F16):
         return call("fftconv_quantize_blocks", x, ld, q, s, t, k, dtype, None)
-    for kw in (dict(x=None), dict(q=None), dict(s=None), dict(ld=63), dict(ld=1 << 40), dict(dtype=9), dict(s=A + 1), dict(x=A + 1), dict(k=0), dict(t=-1), dict(t=1 << 31)):
+    for kw in (dict(x=None), dict(q=None), dict(s=None), dict(ld=63), dict(ld=1 << 60), dict(dtype=9), dict(s=A + 1), dict(x=A + 1), dict(k=0), dict(t=-1), dict(t=1 << 31)):
         assert rows(**kw) == EINVAL, kw
     assert rows(k=1 << 21, ld=1 << 21) == EUNSUPPORTED and rows(t=0, x=None) == OK
 
