@@ -16,13 +16,20 @@ __device__ __forceinline__ int quotient(int x, int d, uint32_t by_d)
 }
 static uint32_t reciprocal(int64_t d) { return d > 1 ? (uint32_t)((((int64_t)1 << 32) + d - 1) / d) : 0; }
 
-// 16 bytes of a row of K from column k on; what lies beyond K reads as zero.
+// 16 bytes of a row of K from column k on; what lies beyond K reads as zero. The row's end is its last 16 bytes, moved down (a load for every byte: a product of
+// 5950 x 63 -> 10176 took 141 us instead of 83).
 __device__ __forceinline__ uint4 load16(const void *bytes, int64_t k, int64_t K)
 {
     const uint8_t *const row = (const uint8_t *)bytes;
     uint4 v = make_uint4(0, 0, 0, 0);
     if (k + 16 <= K) {
         __builtin_memcpy(&v, row + k, 16);
+    } else if (k < K && K >= 16) {
+        uint64_t w[2];
+        __builtin_memcpy(w, row + K - 16, 16);
+        const int past = (int)(k + 16 - K) * 8;              // bits, 8 ... 120
+        const uint64_t lo = past < 64 ? w[0] >> past | w[1] << (64 - past) : w[1] >> (past - 64), hi = past < 64 ? w[1] >> past : 0;
+        v = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
     } else if (k < K) {
         uint32_t w[4] = {};
 #pragma unroll

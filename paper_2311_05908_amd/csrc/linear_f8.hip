@@ -682,11 +682,12 @@ template <typename T> __global__ void __launch_bounds__(256) k_f8_sums(const F8A
 }
 
 // Rows whose length is no multiple of 16 are laid out again at a distance that is one, with zeros behind them, tokens and weight one after the other, where
-// the products are worth the bytes and another launch. In us, as they are and so: 4095 -> 4096 64 tokens 44 and 23, 300 67 and 33, 8192 386 and 161; 8191 -> 1000
-// 100 tokens 60 and 24, 64 tokens 78 either way; 2047 -> 4096 100 tokens 29 and 23; but 1001 -> 3001 300 tokens 14 and 20, 512 16 and 24, 2048 34 and 26.
+// that is worth the bytes and another launch: rows of 2000 and T O K of 2^29 and more, or 2^22 results. In us, as they are and so: 4095 -> 4096 64 tokens 44 and
+// 23, 300 67 and 33, 8192 386 and 161; 8191 -> 1000 100 tokens 60 and 24, 64 tokens 78 either way; 2047 -> 4096 100 tokens 29 and 23; 1001 -> 3001 2048
+// tokens 34 and 26, but 300 14 and 20, 512 16 and 24; 63 -> 10176 5950 tokens 83 and 35.
 static bool f8_padded(int64_t T, int64_t K, int64_t O)
 {
-    return T > 16 && K % 16 != 0 && (double)T * (double)O * (double)K >= (double)((int64_t)1 << (K >= 2000 ? 29 : 32));
+    return T > 16 && K % 16 != 0 && (T >= (((int64_t)1 << 22) + O - 1) / O || (K >= 2000 && (double)T * (double)O * (double)K >= (double)((int64_t)1 << 29)));
 }
 struct PadArgs {
     const uint8_t *x, *w;

@@ -190,7 +190,7 @@ def operands(g, b, n, k, o, bias=True):
 
 SHAPES = [(1, 1, 1, 1), (1, 1, 128, 16), (1, 1, 4096, 4096), (2, 1, 129, 17), (1, 7, 1000, 33), (1, 16, 768, 300), (3, 6, 640, 129), (1, 32, 777, 48), (2, 31, 2048, 160),
           (1, 64, 128, 768), (1, 65, 128, 64), (1, 100, 4096, 512), (1, 70, 2048, 100), (2, 128, 256, 256), (1, 200, 1000, 300), (1, 129, 16, 130), (3, 333, 272, 384),
-          (1, 1024, 768, 2304), (2, 1000, 144, 2000), (1, 2100, 528, 2050), (5, 257, 1041, 515), (1, 2048, 384, 2048), (2, 2048, 768, 4608), (4, 1111, 400, 4099)]
+          (1, 1024, 768, 2304), (2, 1000, 144, 2000), (1, 2100, 528, 2050), (5, 257, 1041, 515), (1, 2048, 384, 2048), (2, 2048, 768, 4608), (4, 1111, 400, 4099), (1, 2100, 37, 2050), (3, 700, 15, 2001), (1, 60, 1001, 70001)]
 
 
 @pytest.mark.parametrize("dtype", list(DT))
