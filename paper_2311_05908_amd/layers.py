@@ -327,7 +327,16 @@ _GATES = {"sigmoid": 0, "log": 1}
 
 
 def _scanned(u, w, v, lengths, gate):
-    """(b, c, n), dtype, code and gate of a scan's operands."""
+    """(b, c, n), dtype, code and gate of a scan's operands. (All checks together; what does not pass is gone through once more for what is wrong with it.)"""
+    try:
+        shape, dtype, device = u.shape, u.dtype, _device()
+        if (len(shape) == 3 and shape[1] >= 1 and shape[2] >= 1 and w.shape == shape and w.dtype == dtype and u.is_contiguous() and w.is_contiguous()
+                and u.get_device() == w.get_device() == device
+                and (v is None or (v.shape == shape and v.dtype == dtype and v.is_contiguous() and v.get_device() == device))
+                and (lengths is None or (lengths.dtype == torch.int32 and lengths.shape == shape[:1] and lengths.is_contiguous() and lengths.get_device() == device))):
+            return shape, dtype, _CODE[dtype], _GATES[gate]
+    except (AttributeError, TypeError, KeyError):
+        pass
     _contiguous("u", u, _IO, 3)
     shape, dtype = u.shape, u.dtype
     _contiguous("w", w, (dtype,), 3, shape)
@@ -352,12 +361,12 @@ def gated_scan(u, w, v=None, state=None, lengths=None, gate: str = "sigmoid", ke
     if state is not None:
         _contiguous("state", state, _F32, 2, (b, c))
     y = torch.empty_like(u)
-    last = _empty((b, c), dtype=torch.float32, device=u.device)
-    kept = _empty((b, c, -(-n // 512)), dtype=torch.float32, device=u.device) if keep else None
+    last = u.new_empty((b, c), dtype=torch.float32)
+    kept = u.new_empty((b, c, -(-n // 512)), dtype=torch.float32) if keep else None
     if b:
         lib = _f.load()
         need = _workspace(lib, "gated_scan", b, c, n, code)
-        ws = _empty(need, dtype=torch.uint8, device=u.device) if need else None
+        ws = u.new_empty(need, dtype=torch.uint8) if need else None
         rc = _calls(lib).gated_scan(u.data_ptr(), w.data_ptr(), _ptr(v), _ptr(state), _ptr(lengths), y.data_ptr(), last.data_ptr(), _ptr(kept), b, c, n,
                                     kind, code, _ptr(ws), _f._stream_ptr())
         if rc:
@@ -374,12 +383,12 @@ def gated_scan_backward(dy, u, w, kept, v=None, dlast=None, lengths=None, gate: 
     _contiguous("kept", kept, _F32, 3, (b, c, -(-n // 512)))
     if dlast is not None:
         _contiguous("dlast", dlast, _F32, 2, (b, c))
-    d = _empty((2 if v is None else 3, b, c, n), dtype=dtype, device=u.device)
-    dstate = _empty((b, c), dtype=torch.float32, device=u.device)
+    d = u.new_empty((2 if v is None else 3, b, c, n))
+    dstate = u.new_empty((b, c), dtype=torch.float32)
     if b:
         lib = _f.load()
         need = _workspace(lib, "gated_scan", b, c, n, code)
-        ws = _empty(need, dtype=torch.uint8, device=u.device) if need else None
+        ws = u.new_empty(need, dtype=torch.uint8) if need else None
         at, size = d.data_ptr(), dy.numel() * dy.element_size()
         rc = _calls(lib).gated_scan_backward(dy.data_ptr(), u.data_ptr(), w.data_ptr(), _ptr(v), kept.data_ptr(), _ptr(dlast), _ptr(lengths), at,
                                              at + size, None if v is None else at + 2 * size, dstate.data_ptr(), b, c, n, kind, code, _ptr(ws),
@@ -392,22 +401,30 @@ def gated_scan_backward(dy, u, w, kept, v=None, dlast=None, lengths=None, gate: 
 def gated_step(u, w, state, v=None, gate: str = "sigmoid", out=None):
     """fftconv_gated_step: y of one sample for every channel, u, w, v and state of one shape ((b, c), say). The state after it replaces `state`, or
     goes to `out`, where both have to be kept."""
-    _contiguous("u", u, _IO)
-    shape, dtype = u.shape, u.dtype
-    _contiguous("w", w, (dtype,), None, shape)
-    if v is not None:
-        _contiguous("v", v, (dtype,), None, shape)
-    _contiguous("state", state, _F32, None, shape)
     if out is None:
         out = state
-    elif out is not state:
+    try:
+        shape, dtype, device = u.shape, u.dtype, _device()
+        code, kind = _CODE[dtype], _GATES[gate]
+        good = (w.shape == state.shape == out.shape == shape and w.dtype == dtype and state.dtype == out.dtype == torch.float32 and u.is_contiguous()
+                and w.is_contiguous() and state.is_contiguous() and out.is_contiguous()
+                and u.get_device() == w.get_device() == state.get_device() == out.get_device() == device
+                and (v is None or (v.shape == shape and v.dtype == dtype and v.is_contiguous() and v.get_device() == device)))
+    except (AttributeError, TypeError, KeyError):
+        good = False
+    if not good:                                  # one after the other, for what is wrong
+        _contiguous("u", u, _IO)
+        shape, dtype = u.shape, u.dtype
+        _contiguous("w", w, (dtype,), None, shape)
+        if v is not None:
+            _contiguous("v", v, (dtype,), None, shape)
+        _contiguous("state", state, _F32, None, shape)
         _contiguous("out", out, _F32, None, shape)
-    if gate not in _GATES:
         raise ValueError("gate is \"sigmoid\" or \"log\"")
     y = torch.empty_like(u)
     t = y.numel()
     if t:
-        rc = _calls(_f.load()).gated_step(u.data_ptr(), w.data_ptr(), _ptr(v), state.data_ptr(), out.data_ptr(), y.data_ptr(), t, _GATES[gate], _CODE[dtype],
+        rc = _calls(_f.load()).gated_step(u.data_ptr(), w.data_ptr(), _ptr(v), state.data_ptr(), out.data_ptr(), y.data_ptr(), t, kind, code,
                                           _f._stream_ptr())
         if rc:
             _f._check(rc)
