@@ -394,7 +394,7 @@ template <typename T, bool CHANNELS> __global__ void __launch_bounds__(512, 2) k
         }
         int lane = threadIdx.x & 63;
         asm volatile("" : "+v"(lane));                           // (else the compiler keeps the places below in registers throughout the sums)
-        const int l32 = lane & 31, half = lane >> 5, r0 = tr * BR, s0 = ts * BS;
+        const int l32 = lane & 31, r0 = tr * BR, s0 = ts * BS;
         const int r1 = r0 + wr * FR * 32, s1 = s0 + wsv * FS * 32;
         // All of it inside y, in one sequence and one part of y: places are linear in rows and columns.
         bool whole = r0 + BR <= a.O && s0 + BS <= a.T && (CHANNELS ? a.N : a.O) < 1 << 26;        // (32-bit distances of seven rows)
@@ -717,58 +717,69 @@ static int f8_ranges(int64_t T, int64_t K, int64_t O)
     return (int)((blocks + per - 1) / per);
 }
 
-// Few tokens (up to 16 NT): what counts is how fast the weight streams in, so its rows go from memory straight into the operand registers, sixteen
-// rows to a workgroup, whose waves divide the blocks of k among themselves and add their sums up in LDS. Measured: 1 x 4096 -> 4096 5.3 us, 3.2 TB/s of the
-// weight's 16.8 MB, of which a launch is about half.
-template <typename T, int NT> __global__ void __launch_bounds__(512) k_f8_few(const F8Args a)
+// Few tokens (up to 16 NT): what counts is how fast the weight streams in, so its rows go from memory straight into the operand registers, 16 NO to a wave. WK
+// waves divide the blocks of k among themselves and add their sums up in LDS; the eight of a workgroup take 8 / WK such runs of outputs. More outputs to a
+// wave (a token's row is then read less often) and fewer waves to a row (short rows) where enough workgroups are left. Measured: 1 x 4096 -> 4096 5.2 us, 3.2 TB/s
+// of the weight's 16.8 MB, of which a launch is about half; 1 x 8192 -> 16384 27 us, 4.9 TB/s. Against one run of 16 outputs to a workgroup of eight waves:
+// 2048 -> 65536 of 1 token 35 -> 25 us, of 33 78 -> 40, of 64 98 -> 46; 4096 -> 16384 of 33 38 -> 19; 8192 -> 16384 of 64 81 -> 37. With 17 tokens or more and few
+// outputs the tokens' rows bound it, which every workgroup reads whole: 64 x 16384 -> 4096 40 us.
+template <typename T, int NT, int NO, int WK> __global__ void __launch_bounds__(512) k_f8_few(const F8Args a)
 {
-    __shared__ f32x4 sums[8][NT][64];
+    __shared__ f32x4 sums[8][NO * NT][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
-    const int64_t o0 = ((int64_t)a.first + blockIdx.x) * 16;
-    const uint8_t *const w = a.w + min(o0 + l16, (int64_t)a.O - 1) * a.K;
-    const float *const ws = a.ws + o0 / 128 * a.blocks;
-    const uint8_t *x[NT];
+    constexpr int RUNS = 8 / WK;
+    static_assert(RUNS * NO <= 8, "a workgroup's outputs lie in one tile of the weight");
+    const int64_t wg0 = ((int64_t)a.first + blockIdx.x) * (16 * NO * RUNS), o0 = wg0 + wave / WK * (16 * NO);
+    const float *const ws = a.ws + wg0 / 128 * a.blocks;
+    const uint8_t *x[NT], *w[NO];
     int t[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) t[j] = min(j * 16 + l16, a.T - 1), x[j] = a.x + (int64_t)t[j] * a.K;
-    f32x4 acc[NT] = {};
-    constexpr int U = NT == 1 ? 4 : 2;
-    for (int k0 = wave; k0 < a.blocks; k0 += 8 * U) {
-        Half fw[U], fx[U][NT];
+#pragma unroll
+    for (int i = 0; i < NO; ++i) w[i] = a.w + min(o0 + 16 * i + l16, (int64_t)a.O - 1) * a.K;
+    f32x4 acc[NO][NT] = {};
+    constexpr int U = NT == 1 ? 4 : NT * NO >= 8 ? 1 : 2;
+    for (int k0 = wave % WK; k0 < a.blocks; k0 += WK * U) {
+        Half fw[U][NO], fx[U][NT];
         float s[U][NT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t k = (int64_t)(k0 + 8 * u) * 128 + quarter * 16;
-            const int block = min(k0 + 8 * u, a.blocks - 1);
-            fw[u] = {load16(w, k, a.K), load16(w, k + 64, a.K)};
+            const int64_t k = (int64_t)(k0 + WK * u) * 128 + quarter * 16;
+            const int block = min(k0 + WK * u, a.blocks - 1);
+#pragma unroll
+            for (int i = 0; i < NO; ++i) fw[u][i] = {load16(w[i], k, a.K), load16(w[i], k + 64, a.K)};
             const float sw = ws[block];
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 fx[u][j] = {load16(x[j], k, a.K), load16(x[j], k + 64, a.K)};
                 // (a block beyond the last is one of zeros)
-                s[u][j] = k0 + 8 * u < a.blocks ? a.xs[(int64_t)block * a.T + t[j]] * sw : 0.f;
+                s[u][j] = k0 + WK * u < a.blocks ? a.xs[(int64_t)block * a.T + t[j]] * sw : 0.f;
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const f32x4 p = products16<sizeof(T) == 4>(fw[u], fx[u][j]);
+            for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(p[e], s[u][j], acc[j][e]);
-            }
+                for (int i = 0; i < NO; ++i) {
+                    const f32x4 p = products16<sizeof(T) == 4>(fw[u][i], fx[u][j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], s[u][j], acc[i][j][e]);
+                }
     }
 #pragma unroll
-    for (int j = 0; j < NT; ++j) sums[wave][j][lane] = acc[j];
+    for (int i = 0; i < NO; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
     lds_barrier();
     // lane l holds token l % 16 of the sixteen, outputs 4 (l / 16) ... + 3
-    for (int i = threadIdx.x; i < NT * 256; i += 512) {
-        const int e = i & 3, l = (i >> 2) & 63, j = i >> 8;
+    for (int i = threadIdx.x; i < RUNS * NO * NT * 256; i += 512) {
+        const int e = i & 3, l = (i >> 2) & 63, tile = (i >> 8) % (NO * NT), r = (i >> 8) / (NO * NT);
         float sum = 0.f;
 #pragma unroll
-        for (int v = 0; v < 8; ++v) sum += sums[v][j][l][e];
-        const int token = j * 16 + (l & 15);
-        const int64_t o = o0 + 4 * (l >> 4) + e;
+        for (int v = 0; v < WK; ++v) sum += sums[r * WK + v][tile][l][e];
+        const int token = tile % NT * 16 + (l & 15);
+        const int64_t o = wg0 + (r * NO + tile / NT) * 16 + 4 * (l >> 4) + e;
         if (token >= a.T || o >= a.O) continue;
         ((T *)a.y)[token_of(a, token) + output_of(a, (int)o)] = from_f32<T>(sum + (a.bias ? a.bias[o] : 0.f));
     }
@@ -792,14 +803,22 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
         workspace = p.to + rows * p.pitch;
     }
     if (a.T <= 64) {
-        return in_pieces(((int64_t)a.O + 15) / 16, 512, [&](int64_t first, unsigned g) -> int {
-            a.first = (int)first;
-            if (a.T <= 16) k_f8_few<T, 1><<<g, 512, 0, s>>>(a);
-            else if (a.T <= 32) k_f8_few<T, 2><<<g, 512, 0, s>>>(a);
-            else k_f8_few<T, 4><<<g, 512, 0, s>>>(a);
-            FC_HIP(hipGetLastError());
-            return FFTCONV_OK;
-        });
+        auto few = [&](auto kernel, int64_t outputs) -> int {
+            return in_pieces((a.O + outputs - 1) / outputs, 512, [&](int64_t first, unsigned g) -> int {
+                a.first = (int)first;
+                kernel<<<g, 512, 0, s>>>(a);
+                FC_HIP(hipGetLastError());
+                return FFTCONV_OK;
+            });
+        };
+        const int64_t runs = ((int64_t)a.O + 15) / 16;           // of 16 outputs; 256 workgroups at least are wanted
+        if (a.T <= 16) {
+            if (a.blocks <= 8 && runs >= 4 * 256) return few(k_f8_few<T, 1, 1, 2>, 64);
+            if (a.blocks <= 16 && runs >= 2 * 256) return few(k_f8_few<T, 1, 1, 4>, 32);
+            return few(k_f8_few<T, 1, 1, 8>, 16);
+        }
+        if (a.T <= 32) return runs >= 2 * 256 ? few(k_f8_few<T, 2, 2, 8>, 32) : few(k_f8_few<T, 2, 1, 8>, 16);
+        return runs >= 4 * 256 ? few(k_f8_few<T, 4, 4, 8>, 64) : runs >= 2 * 256 ? few(k_f8_few<T, 4, 2, 8>, 32) : few(k_f8_few<T, 4, 1, 8>, 16);
     }
     auto launch = [&](auto f) -> int {
         constexpr int F = decltype(f)::value, lds = 2 * 2 * 64 * F * 128;

@@ -242,6 +242,17 @@ def test_ranges_and_long_rows(t, k, o, dtype):
     within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
 
 
+# Outputs and waves to a row by their number, the blocks of k and the tokens, each with an end inside a workgroup's outputs.
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t", [1, 15, 17, 32, 33, 64])
+@pytest.mark.parametrize("k,o", [(1, 16369), (130, 16400), (1000, 16500), (1025, 16401), (1040, 8177), (2048, 8200), (2049, 8209), (3000, 33001)])
+def test_few_tokens_of_many_outputs(t, k, o, dtype):
+    rows, weight, bias = operands(gen(k + o + t), 1, t, k, o)
+    value, bound = product(rows, weight, bias)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype]), value, bound, dtype)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
+
+
 def test_sums_are_as_fine_as_fp32():
     """Blocks whose products cancel but for one: 448^2 = 49 2^12 and 2^-2 add up within fp32's 24 bits, so what remains is exact, where
     products that keep 13 bits below the largest leave nothing."""
