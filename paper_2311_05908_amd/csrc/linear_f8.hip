@@ -7,7 +7,7 @@
 // number a lane, and the weight's scale is the same in the whole wave. Token by token a lane's four consecutive rows are neighbours in y; channel by
 // channel the lanes are.
 //
-// Which kernel: up to 64 tokens k_f8_few, bound by the weight's bytes. Above, with k in pieces of 16 bytes (both operands aligned to them), k_f8_large on
+// Which kernel: up to 64 tokens k_f8_few, bound by the weight's bytes, but for very long rows and very many outputs. Above, with k in pieces of 16 bytes (both operands aligned to them), k_f8_large on
 // tiles of 256 x 256 where these fill the compute units, else k_f8_small on 128 x 128 where there are 128 of those, or with k in ranges where there
 // are fewer and k is 1024 or more. Rows of other lengths are laid out again for these where that pays (f8_padded); everything else is k_f8's, which
 // takes any k at any alignment.
@@ -706,11 +706,15 @@ __global__ void __launch_bounds__(256) k_f8_pad(const PadArgs a)
     *(uint4 *)(a.to + row * a.pitch + p * 16) = v;
 }
 
-// Into how many ranges k goes: where few tiles are left for the compute units, as many as give each one, of four blocks at least.
+// Into how many ranges k goes: where few tiles are left for the compute units, as many as give each one, of four blocks at least. Up to 64 tokens where that is
+// faster than k_f8_few, which takes the longer the more blocks and sixteens of tokens there are, however few the outputs. In us, k_f8_few and ranges: 33 tokens,
+// 8192 -> 4096 17.7 and 15.6, 4096 -> 4096 9.6 and 13.5; 17 tokens, 16384 -> 4096 25.3 and 20.9, 8192 -> 4096 12.5 and 15.3; one, 32768 -> 1024 25.8 and 20.3,
+// 12288 -> 1024 10.4 and 15.2; 64 of 65536 -> 1024 148 and 29.
 static int f8_ranges(int64_t T, int64_t K, int64_t O)
 {
     const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128), blocks = (K + 127) / 128;
-    if (T <= 64 || (K % 16 != 0 && !f8_padded(T, K, O)) || tiles >= 128) return 1;
+    if (T <= 64 && blocks * (T <= 16 ? 1 : T <= 32 ? 2 : 4) < 256) return 1;
+    if ((K % 16 != 0 && !f8_padded(T, K, O)) || tiles >= 128) return 1;
     const int64_t most = 256 / tiles < blocks / 4 ? 256 / tiles : blocks / 4;
     if (most < 2) return 1;
     const int64_t per = (blocks + most - 1) / most;
@@ -721,8 +725,7 @@ static int f8_ranges(int64_t T, int64_t K, int64_t O)
 // waves divide the blocks of k among themselves and add their sums up in LDS; the eight of a workgroup take 8 / WK such runs of outputs. More outputs to a
 // wave (a token's row is then read less often) and fewer waves to a row (short rows) where enough workgroups are left. Measured: 1 x 4096 -> 4096 5.2 us, 3.2 TB/s
 // of the weight's 16.8 MB, of which a launch is about half; 1 x 8192 -> 16384 27 us, 4.9 TB/s. Against one run of 16 outputs to a workgroup of eight waves:
-// 2048 -> 65536 of 1 token 35 -> 25 us, of 33 78 -> 40, of 64 98 -> 46; 4096 -> 16384 of 33 38 -> 19; 8192 -> 16384 of 64 81 -> 37. With 17 tokens or more and few
-// outputs the tokens' rows bound it, which every workgroup reads whole: 64 x 16384 -> 4096 40 us.
+// 2048 -> 65536 of 1 token 35 -> 25 us; 4096 -> 16384 of 33 38 -> 19; 8192 -> 16384 of 64 81 -> 37.
 template <typename T, int NT, int NO, int WK> __global__ void __launch_bounds__(512) k_f8_few(const F8Args a)
 {
     __shared__ f32x4 sums[8][NO * NT][64];
@@ -802,7 +805,11 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
         a.x = p.to, a.w = p.to + a.T * p.pitch, a.K = p.pitch, pieces = true;
         workspace = p.to + rows * p.pitch;
     }
-    if (a.T <= 64) {
+    auto tiles = [&](int64_t b) { return ((a.O + b - 1) / b) * ((a.T + b - 1) / b); };
+    // Up to 64 tokens: in ranges where these are the faster, or on tiles where those fill the compute units, once or twice. In us, k_f8_few and tiles: 64 tokens,
+    // 2048 -> 33000 33 and 24, 4096 -> 16384 21 and 27; 32 tokens, 2048 -> 65536 36 and 26, 8192 -> 40000 91 and 94; one, 1024 -> 65536 14 and 16; fp32,
+    // 32 tokens, 2048 -> 65536 48 and 39.
+    if (a.T <= 64 && !(pieces && (a.ranges > 1 || (a.T > 16 && tiles(128) >= (a.T > 32 ? 256 : 512))))) {
         auto few = [&](auto kernel, int64_t outputs) -> int {
             return in_pieces((a.O + outputs - 1) / outputs, 512, [&](int64_t first, unsigned g) -> int {
                 a.first = (int)first;
@@ -840,7 +847,6 @@ template <typename T> static int run(F8Args &a, void *workspace, hipStream_t s)
         return FFTCONV_OK;
     };
     constexpr int LARGE_LDS = 2 * 512 * 128 + 8 * (2 * 512 + 512), SMALL_LDS = 4 * 256 * 64 + 8 * (4 * 256 + 256);
-    auto tiles = [&](int64_t b) { return ((a.O + b - 1) / b) * ((a.T + b - 1) / b); };
     using std::integral_constant;
     if (pieces && a.ranges > 1) {
         a.per = (a.blocks + a.ranges - 1) / a.ranges, a.part = (float *)workspace;

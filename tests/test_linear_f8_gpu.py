@@ -253,6 +253,20 @@ def test_few_tokens_of_many_outputs(t, k, o, dtype):
     within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
 
 
+# On both sides of where few tokens go by ranges of k or by tiles.
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t,k,o", [(1, 32768, 40), (16, 32656, 130), (16, 32640, 130), (17, 16384, 200), (32, 16256, 129), (17, 16384 + 48, 8000), (33, 8192, 257), (64, 8064, 1000),
+                                   (64, 8208, 8000), (50, 8001, 300), (40, 512, 32641), (64, 272, 32640), (33, 16, 40000), (20, 256, 65409), (32, 400, 65400), (16, 512, 65500)])
+def test_few_tokens_in_ranges_and_tiles(t, k, o, dtype):
+    rows, weight, bias = operands(gen(k + o + t), 1, t, k, o)
+    value, bound = product(rows, weight, bias)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype]), value, bound, dtype)
+    within(layers.linear_f8(rows, weight, bias=bias, dtype=DT[dtype], layout="channels"), laid(value, 1), laid(bound, 1), dtype)
+    at = torch.empty(weight.q.numel() + 3, dtype=F8, device="cuda")[3:].view(o, k)          # (at an odd address: by neither)
+    at.copy_(weight.q)
+    within(layers.linear_f8(rows, weight._replace(q=at), bias=bias, dtype=DT[dtype]), value, bound, dtype)
+
+
 def test_sums_are_as_fine_as_fp32():
     """Blocks whose products cancel but for one: 448^2 = 49 2^12 and 2^-2 add up within fp32's 24 bits, so what remains is exact, where
     products that keep 13 bits below the largest leave nothing."""

@@ -19,7 +19,7 @@ def test_operators_of_a_recurrent_layer_agree_bit_for_bit(monkeypatch):
 
     # (rows, samples, k, outputs, parts)
     shapes = [(4, 4096, 768, 2304, 3), (2, 2048, 768, 2304, 3), (1, 8190, 528, 4000, 1), (1, 100, 4096, 2048, 2), (1, 5, 1000, 100, 1), (1, 777, 333, 555, 1), (3, 999, 400, 600, 2),
-              (1, 1, 700, 16400, 1), (1, 9, 1100, 8200, 1), (1, 20, 300, 8200, 1), (1, 50, 300, 8200, 2), (1, 50, 300, 16400, 2)]
+              (1, 1, 700, 16400, 1), (1, 9, 1100, 8200, 1), (1, 20, 300, 8200, 1), (1, 50, 300, 8200, 2), (1, 50, 300, 16400, 2), (1, 40, 8192, 300, 1), (1, 40, 256, 33000, 1)]
     cases = [(normal(b, n, k), normal(o, k), parts) for b, n, k, o, parts in shapes]
     u, w, v, dy = (normal(3, 40, 5000) for _ in range(4))
     grads = [normal(1000), normal(300, 77)]
