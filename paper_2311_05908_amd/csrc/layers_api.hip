@@ -24,6 +24,24 @@ bool aligned(const void *p, int64_t to) { return ((uintptr_t)p & (uintptr_t)(to 
 // a * b for non-negative numbers, or -1 where it is over `most`
 int64_t times(int64_t a, int64_t b, int64_t most = MOST) { return a < 0 || b < 0 || (a > 0 && b > most / a) ? -1 : a * b; }
 
+// What a call reads or writes; nothing where `at` is NULL.
+struct Place {
+    const void *at;
+    int64_t bytes;
+};
+bool meet(const Place &a, const Place &b)
+{
+    return a.at && b.at && (uintptr_t)a.at < (uintptr_t)b.at + (uintptr_t)b.bytes && (uintptr_t)b.at < (uintptr_t)a.at + (uintptr_t)a.bytes;
+}
+// Whether one of the first `written` places meets another one.
+template <int N> bool overlap(const Place (&p)[N], int written)
+{
+    for (int i = 0; i < written; ++i)
+        for (int j = i + 1; j < N; ++j)
+            if (meet(p[i], p[j])) return true;
+    return false;
+}
+
 int check_rows(const char *who, const void *x, int64_t ldx, int64_t T, int64_t D, int dtype)
 {
     if (!known(dtype)) return bad(who, "unknown dtype");
@@ -256,8 +274,8 @@ int fftconv_gated_step(const void *u, const void *w, const void *v, const float 
     const int64_t to = size_of(dtype);
     if (!aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(y, to) || !aligned(state, 4) || !aligned(next, 4))
         return bad(who, "a tensor is not aligned to its elements");
-    if (next != state && (uintptr_t)next < (uintptr_t)(state + T) && (uintptr_t)state < (uintptr_t)(next + T))
-        return bad(who, "next overlaps state without being it");
+    const Place places[] = {{next, 4 * T}, {y, to * T}, {u, to * T}, {w, to * T}, {v, to * T}, {next == state ? nullptr : state, 4 * T}};
+    if (overlap(places, 2)) return bad(who, "a result overlaps another tensor (next may be state itself)");
     return lay::gated_step(u, w, v, state, next, y, T, gate, dtype, (hipStream_t)stream);
 }
 

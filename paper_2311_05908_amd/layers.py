@@ -400,7 +400,7 @@ def gated_scan_backward(dy, u, w, kept, v=None, dlast=None, lengths=None, gate: 
 
 def gated_step(u, w, state, v=None, gate: str = "sigmoid", out=None):
     """fftconv_gated_step: y of one sample for every channel, u, w, v and state of one shape ((b, c), say). The state after it replaces `state`, or
-    goes to `out`, where both have to be kept."""
+    goes to `out`, where both have to be kept; `out` overlaps none of the others."""
     if out is None:
         out = state
     try:
