@@ -319,7 +319,8 @@ int fftconv_linear_grad_weight(const void *dy, const int8_t *q, const float *sca
  *   h is recomputed from u, w and kept.  dv is NULL exactly where v is; dstate may be NULL.  Gradients behind a sequence's end are zero.
  * fftconv_gated_step: one sample for each of T = B C channels: next = a state + x, y = v next.  next may be state itself; apart from
  *   that no result overlaps another tensor (refused).
- *   B C below 2^31, N below 2^31; workspace: fftconv_workspace_bytes_gated_scan bytes for either pass (may be NULL when that is 0). */
+ *   B C below 2^31, N below 2^31; workspace: fftconv_workspace_bytes_gated_scan bytes for either pass (may be NULL when that is 0).  Results and
+ *   workspace of either pass overlap nothing else, `last` not `state` either (refused): a row may go to several workgroups. */
 enum { FFTCONV_GATE_SIGMOID = 0, FFTCONV_GATE_LOG = 1 };
 size_t fftconv_workspace_bytes_gated_scan(int64_t B, int64_t C, int64_t N, int dtype);
 int fftconv_gated_scan(const void *u, const void *w, const void *v, const float *state, const int32_t *lengths, void *y, float *last, float *kept,

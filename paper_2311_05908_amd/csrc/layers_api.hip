@@ -24,14 +24,14 @@ bool aligned(const void *p, int64_t to) { return ((uintptr_t)p & (uintptr_t)(to 
 // a * b for non-negative numbers, or -1 where it is over `most`
 int64_t times(int64_t a, int64_t b, int64_t most = MOST) { return a < 0 || b < 0 || (a > 0 && b > most / a) ? -1 : a * b; }
 
-// What a call reads or writes; nothing where `at` is NULL.
+// What a call reads or writes; nothing where `at` is NULL, or of no bytes.
 struct Place {
     const void *at;
     int64_t bytes;
 };
 bool meet(const Place &a, const Place &b)
 {
-    return a.at && b.at && (uintptr_t)a.at < (uintptr_t)b.at + (uintptr_t)b.bytes && (uintptr_t)b.at < (uintptr_t)a.at + (uintptr_t)a.bytes;
+    return a.at && b.at && a.bytes > 0 && b.bytes > 0 && (uintptr_t)a.at < (uintptr_t)b.at + (uintptr_t)b.bytes && (uintptr_t)b.at < (uintptr_t)a.at + (uintptr_t)a.bytes;
 }
 // Whether one of the first `written` places meets another one.
 template <int N> bool overlap(const Place (&p)[N], int written)
@@ -243,7 +243,10 @@ int fftconv_gated_scan(const void *u, const void *w, const void *v, const float 
     if (!aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(y, to) || !aligned(state, 4) || !aligned(lengths, 4) || !aligned(last, 4) ||
         !aligned(kept, 4) || !aligned(workspace, 8))
         return bad(who, "a tensor is not aligned to its elements");
-    if (!workspace && lay::gated_scan_workspace(B * C, N) != 0) return bad(who, "the workspace is NULL");
+    const int64_t work = (int64_t)lay::gated_scan_workspace(B * C, N), rows = 4 * B * C, all = to * B * C * N;
+    if (!workspace && work != 0) return bad(who, "the workspace is NULL");
+    const Place places[] = {{y, all}, {last, rows}, {kept, rows * ((N + 511) / 512)}, {workspace, work}, {u, all}, {w, all}, {v, all}, {state, rows}, {lengths, 4 * B}};
+    if (overlap(places, 4)) return bad(who, "a result or the workspace overlaps another tensor");
     return lay::gated_scan(u, w, v, state, lengths, y, last, kept, B, C, N, gate, dtype, workspace, (hipStream_t)stream);
 }
 
@@ -260,7 +263,11 @@ int fftconv_gated_scan_backward(const void *dy, const void *u, const void *w, co
     if (!aligned(dy, to) || !aligned(u, to) || !aligned(w, to) || !aligned(v, to) || !aligned(du, to) || !aligned(dw, to) || !aligned(dv, to) ||
         !aligned(kept, 4) || !aligned(dlast, 4) || !aligned(lengths, 4) || !aligned(dstate, 4) || !aligned(workspace, 8))
         return bad(who, "a tensor is not aligned to its elements");
-    if (!workspace && lay::gated_scan_workspace(B * C, N) != 0) return bad(who, "the workspace is NULL");
+    const int64_t work = (int64_t)lay::gated_scan_workspace(B * C, N), rows = 4 * B * C, all = to * B * C * N;
+    if (!workspace && work != 0) return bad(who, "the workspace is NULL");
+    const Place places[] = {{du, all}, {dw, all}, {dv, all}, {dstate, rows}, {workspace, work}, {dy, all}, {u, all}, {w, all}, {v, all}, {kept, rows * ((N + 511) / 512)},
+                            {dlast, rows}, {lengths, 4 * B}};
+    if (overlap(places, 5)) return bad(who, "a result or the workspace overlaps another tensor");
     return lay::gated_scan_backward(dy, u, w, v, kept, dlast, lengths, du, dw, dv, dstate, B, C, N, gate, dtype, workspace, (hipStream_t)stream);
 }
 

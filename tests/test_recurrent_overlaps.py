@@ -49,3 +49,45 @@ def test_step_in_place():
     for name in ("u", "w", "v", "y"):
         step(next=STEP["state"], **{name: STEP["state"]})
         step(next=STEP["state"], **{name: STEP["state"] + 396})
+
+
+SCAN = places("u", "w", "v", "state", "lengths", "y", "last", "kept", "ws")
+BACK = places("dy", "u", "w", "v", "kept", "dlast", "lengths", "du", "dw", "dv", "dstate", "ws")
+B, C, N = 2, 3, 5000          # rows in segments, so that there is a workspace
+
+
+def bytes_of(name, size):
+    if name == "ws":
+        return fftconv.load().fftconv_workspace_bytes_gated_scan(B, C, N, F32)
+    return {"state": 4 * B * C, "last": 4 * B * C, "dlast": 4 * B * C, "dstate": 4 * B * C, "lengths": 4 * B, "kept": 4 * B * C * 10}.get(name, size * B * C * N)
+
+
+def scan(dtype, **moved):
+    p = {**SCAN, **moved}
+    refused("fftconv_gated_scan", *(p[k] for k in ("u", "w", "v", "state", "lengths", "y", "last", "kept")), B, C, N, 0, dtype, p["ws"], None)
+
+
+def back(dtype, **moved):
+    p = {**BACK, **moved}
+    refused("fftconv_gated_scan_backward", *(p[k] for k in ("dy", "u", "w", "v", "kept", "dlast", "lengths", "du", "dw", "dv", "dstate")), B, C, N, 1, dtype, p["ws"], None)
+
+
+@pytest.mark.parametrize("dtype,size", [(F32, 4), (F16, 2)])
+@pytest.mark.parametrize("call,all_of,results", [(scan, SCAN, ("y", "last", "kept", "ws")), (back, BACK, ("du", "dw", "dv", "dstate", "ws"))])
+def test_scans(call, all_of, results, dtype, size):
+    """Every result and the workspace against every other tensor: together, the first 8 bytes on its last, its last on the first. Among them last on state (dstate on
+    dlast), which workgroups of a row's other segments may still have to read."""
+    for result in results:
+        for name in all_of:
+            if name != result:
+                for at in (all_of[name], all_of[name] + bytes_of(name, size) - 8, all_of[name] - bytes_of(result, size) + 8):
+                    call(dtype, **{result: at - at % 8 if result == "ws" else at})
+
+
+def test_scans_without_what_may_be_missing():
+    """What is not there meets nothing; what is there does."""
+    none = dict(v=None, state=None, lengths=None, last=None, kept=None)
+    scan(F32, **none, y=SCAN["u"])
+    scan(BF16, **{**none, "kept": SCAN["w"]})
+    back(F32, v=None, dv=None, dlast=None, lengths=None, dstate=None, du=BACK["dy"])
+    back(F16, v=None, dv=None, lengths=None, dstate=BACK["dlast"])

@@ -41,3 +41,42 @@ def test_step():
     assert torch.equal(layers.gated_step(a, c, d, v=e, out=b), y) and torch.equal(b, out)
     assert all(torch.equal(x, k) for x, k in zip((a, c, e, d), kept))
     assert torch.equal(layers.gated_step(a, c, d, v=e), y) and torch.equal(d, out)          # in place
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("b,c,n", [(2, 3, 5000), (2, 24, 1001)])
+def test_scans_side_by_side(b, c, n, dtype):
+    """Through the C ABI, rows in segments and not: operands, results and workspace in one buffer, each where another ends."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    u, w, v, dy = (torch.randn(b, c, n, generator=g, device="cuda").to(dtype) for _ in range(4))
+    state, dlast = (torch.randn(b, c, generator=g, device="cuda") for _ in range(2))
+    lengths = torch.tensor([n, n // 2], dtype=torch.int32, device="cuda")
+    y, last, kept = layers.gated_scan(u, w, v=v, state=state, lengths=lengths, keep=True)
+    d, dstate = layers.gated_scan_backward(dy, u, w, kept, v=v, dlast=dlast, lengths=lengths)
+    lib, code = fftconv.load(), {torch.float32: 0, torch.bfloat16: 2}[dtype]
+    need = lib.fftconv_workspace_bytes_gated_scan(b, c, n, code)
+    assert (need > 0) == (n == 5000)
+
+    def buffer(*ts):
+        """Stretches of one buffer for tensors (copies) and sizes in bytes, in the order given."""
+        sizes = [t if isinstance(t, int) else t.numel() * t.element_size() for t in ts]
+        store, at, views = torch.full((sum(sizes),), 0xff, dtype=torch.uint8, device="cuda"), 0, []
+        for t, size in zip(ts, sizes):
+            views.append(store[at:at + size])
+            if not isinstance(t, int):
+                views[-1].view(t.dtype).view(t.shape).copy_(t)
+            at += size
+        return views
+
+    all_, rows = u.numel() * u.element_size(), 4 * b * c
+    ws, state_, last_, u_, y_, w_, v_, kept_, lengths_ = buffer(need, state, rows, u, all_, w, v, kept.numel() * 4, lengths)
+    where = [t.data_ptr() for t in (u_, w_, v_, state_, lengths_, y_, last_, kept_)]
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.fftconv_gated_scan(*where, b, c, n, 0, code, ws.data_ptr(), stream) == 0
+    for got, want in ((y_, y), (last_, last), (kept_, kept), (u_, u), (w_, w), (v_, v), (state_, state), (lengths_, lengths)):
+        assert torch.equal(got.view(want.dtype).view(want.shape), want)
+    ws, dlast_, dstate_, dy_, du_, dw_, dv_, u_, w_, v_, kept_, lengths_ = buffer(need, dlast, rows, dy, all_, all_, all_, u, w, v, kept, lengths)
+    where = [t.data_ptr() for t in (dy_, u_, w_, v_, kept_, dlast_, lengths_, du_, dw_, dv_, dstate_)]
+    assert lib.fftconv_gated_scan_backward(*where, b, c, n, 0, code, ws.data_ptr(), stream) == 0
+    for got, want in ((du_, d[0]), (dw_, d[1]), (dv_, d[2]), (dstate_, dstate), (dy_, dy), (u_, u), (w_, w), (v_, v), (kept_, kept), (dlast_, dlast), (lengths_, lengths)):
+        assert torch.equal(got.view(want.dtype).view(want.shape), want)
