@@ -358,9 +358,10 @@ int fftconv_linear_f8(const uint8_t *x, const float *x_scale, const uint8_t *w, 
  *     c = min(1, max_norm / (norm + eps)),   out[i] = c grads[i].
  *   grads, out, counts, dtypes, dtypes_out: arrays in HOST memory, read before the call returns; grads[i], out[i]: contiguous, counts[i] >= 0 values
  *   (up to 2^40; none: the addresses may be NULL), dtypes[i] their type.  out NULL: the norm alone (max_norm and eps are not used).  out[i] may be
- *   grads[i]; apart from that nothing that is written overlaps anything else (one tensor twice in place is refused).  dtypes_out[i]: that of grads[i],
- *   or fp32; NULL: those of grads.  Squares are added in 64 bits, c is rounded to fp32, products are rounded to their type.  In place and with
- *   c = 1 nothing is written.  Where a gradient is NaN, norm is NaN and so is everything; where one is infinite, norm is, and c = 0.
+ *   grads[i]; apart from that nothing that is written (results, norm, workspace) overlaps anything else, a norm that is given among it (refused, as
+ *   is one tensor twice in place).  dtypes_out[i]: that of grads[i], or fp32; NULL: those of grads.  Squares are added in 64 bits, c is rounded
+ *   to fp32, products are rounded to their type.  In place and with c = 1 nothing is written.  Where a gradient is NaN, norm is NaN and so is
+ *   everything; where one is infinite, norm is, and c = 0.
  *   norm: where not NULL, the norm as fp32 goes there.  norm_in: NULL, or a norm (one fp32 on the device) that is taken instead: that of several
  *   devices' gradients, say.  workspace: fftconv_workspace_bytes_clip_grads bytes. */
 size_t fftconv_workspace_bytes_clip_grads(const int64_t *counts, int64_t tensors);

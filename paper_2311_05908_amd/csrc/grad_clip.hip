@@ -182,20 +182,22 @@ static int by_place(const void *a, const void *b)
     return x < y ? -1 : x > y;
 }
 
-// Whether what is written is written once, and read by nothing else. -1: no memory.
-int clip_overlaps(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors)
+// Whether what is written is written once, and read by nothing else: results (each may be its own gradient), the norm and the workspace's sums. A norm that is
+// given is read by every workgroup while others write. -1: no memory.
+int clip_overlaps(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors,
+                  const float *norm_in, const float *norm, const void *workspace)
 {
-    Span *const s = (Span *)malloc(sizeof(Span) * (size_t)(tensors > 0 ? tensors : 1));
+    Span *const s = (Span *)malloc(sizeof(Span) * (size_t)(tensors + 2));
     if (!s) return -1;
     int64_t n = 0;
-    for (int64_t i = 0; i < tensors; ++i)
+    for (int64_t i = 0; out && i < tensors; ++i)
         if (counts[i] > 0) s[n++] = {(uintptr_t)out[i], (uintptr_t)out[i] + (uintptr_t)counts[i] * (types_out[i] == FFTCONV_F32 ? 4 : 2), i};
+    if (norm && norm != norm_in) s[n++] = {(uintptr_t)norm, (uintptr_t)(norm + 1), -1};
+    if (!norm_in) s[n++] = {(uintptr_t)workspace, (uintptr_t)workspace + clip_workspace(counts, tensors), -1};
     qsort(s, (size_t)n, sizeof(Span), by_place);
     int found = 0;
     for (int64_t k = 1; k < n; ++k) found |= s[k].from < s[k - 1].to;
-    for (int64_t i = 0; i < tensors && !found; ++i) {
-        if (counts[i] < 1) continue;
-        const uintptr_t from = (uintptr_t)in[i], to = from + (uintptr_t)counts[i] * (types[i] == FFTCONV_F32 ? 4 : 2);
+    auto read = [&](uintptr_t from, uintptr_t to, int64_t i) {
         int64_t lo = 0, hi = n;                  // spans before lo end at or before `from`
         while (lo < hi) {
             const int64_t mid = (lo + hi) / 2;
@@ -203,7 +205,10 @@ int clip_overlaps(const void *const *in, void *const *out, const int64_t *counts
             else hi = mid;
         }
         for (; lo < n && s[lo].from < to; ++lo) found |= s[lo].i != i || s[lo].from != from || s[lo].to != to;
-    }
+    };
+    for (int64_t i = 0; i < tensors && !found; ++i)
+        if (counts[i] > 0) read((uintptr_t)in[i], (uintptr_t)in[i] + (uintptr_t)counts[i] * (types[i] == FFTCONV_F32 ? 4 : 2), i);
+    if (norm_in) read((uintptr_t)norm_in, (uintptr_t)(norm_in + 1), -2);
     free(s);
     return found;
 }

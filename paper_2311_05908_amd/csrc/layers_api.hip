@@ -374,14 +374,12 @@ int fftconv_clip_grads(const void *const *grads, void *const *out, const int64_t
         if (counts[i] > 0 && (!grads[i] || (out && !out[i]))) return bad(who, "a tensor is NULL");
         if (!aligned(grads[i], size_of(dtypes[i])) || (out && !aligned(out[i], size_of(types_out[i])))) return bad(who, "a tensor is not aligned to its elements");
     }
-    if (out) {
-        const int found = lay::clip_overlaps(grads, out, counts, dtypes, types_out, tensors);
-        if (found < 0) {
-            set_error("%s: no memory", who);
-            return FFTCONV_ENOMEM;
-        }
-        if (found) return bad(who, "a tensor that is written overlaps another one");
+    const int found = lay::clip_overlaps(grads, out, counts, dtypes, types_out, tensors, norm_in, norm, workspace);
+    if (found < 0) {
+        set_error("%s: no memory", who);
+        return FFTCONV_ENOMEM;
     }
+    if (found) return bad(who, "what is written (results, norm, workspace) overlaps something else");
     return lay::clip_grads(grads, out, counts, dtypes, types_out, tensors, max_norm, eps, norm_in, norm, workspace, (hipStream_t)stream);
 }
 

@@ -55,7 +55,8 @@ int linear_f8(const uint8_t *x, const float *xs, const uint8_t *w, const float *
 
 // grad_clip.hip
 size_t clip_workspace(const int64_t *counts, int64_t tensors);
-int clip_overlaps(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors);
+int clip_overlaps(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors,
+                  const float *norm_in, const float *norm, const void *workspace);
 int clip_grads(const void *const *in, void *const *out, const int64_t *counts, const int *types, const int *types_out, int64_t tensors, double limit,
                double eps, const float *norm_in, float *norm, void *workspace, hipStream_t s);
 

@@ -591,5 +591,6 @@ def grad_norm(grads):
 
 def clip_grads(grads, max_norm: float, out=None, norm=None, eps: float = 1e-6):
     """fftconv_clip_grads: every gradient times min(1, max_norm / (norm + eps)), in place, or into `out`, a tensor for each of the same shape and type or
-    in fp32. norm: what grad_norm gave, or the norm over other devices' gradients too, one fp32 on the device; None: that of grads. Returns the norm."""
+    in fp32. norm: what grad_norm gave, or the norm over other devices' gradients too, one fp32 on the device outside of
+    what is written; None: that of grads. Returns the norm."""
     return _clip(grads, float(max_norm), out, norm, float(eps), True)

@@ -2,6 +2,8 @@
 
 Every tensor has a stretch of addresses of its own that are never read; a case moves one of them onto, or partly onto, another. (That tensors side by side are
 taken is tested where there is a device.)"""
+import ctypes
+
 import pytest
 
 from paper_2311_05908_amd import fftconv
@@ -91,3 +93,44 @@ def test_scans_without_what_may_be_missing():
     scan(BF16, **{**none, "kept": SCAN["w"]})
     back(F32, v=None, dv=None, dlast=None, lengths=None, dstate=None, du=BACK["dy"])
     back(F16, v=None, dv=None, lengths=None, dstate=BACK["dlast"])
+
+
+CLIP = places("a", "b", "out a", "out b", "given", "norm", "ws")
+
+
+def clip(out=True, types=(F32, BF16), types_out=(F32, F32), counts=(100, 30), **moved):
+    p = {**CLIP, "given": None, "norm": None, **moved}
+    i64, ints = lambda *v: (ctypes.c_int64 * len(v))(*v), lambda *v: (ctypes.c_int * len(v))(*v)
+    refused("fftconv_clip_grads", i64(p["a"], p["b"]), i64(p["out a"], p["out b"]) if out else None, i64(*counts), ints(*types), ints(*types_out), 2, 1.0, 1e-6,
+            p["given"], p["norm"], p["ws"], None)
+
+
+def test_a_norm_that_is_given_in_what_is_written():
+    """100 values of fp32 and 30 of bf16 into fp32: every workgroup reads the norm while others write."""
+    for name, size in (("out a", 400), ("out b", 120)):
+        for at in (0, 4, size // 2, size - 4):
+            clip(given=CLIP[name] + at, ws=None)
+    for at in (0, 396):                                       # in place
+        clip(given=CLIP["a"] + at, ws=None, **{"out a": CLIP["a"]})
+
+
+def test_a_norm_that_is_written():
+    """On a gradient, a result or the workspace, with clipping and without."""
+    for name, size in (("a", 400), ("b", 60), ("out a", 400), ("out b", 120)):
+        for at in (0, size - 4):
+            clip(norm=CLIP[name] + at)
+            if not name.startswith("out"):
+                clip(norm=CLIP[name] + at, out=False)
+    clip(norm=CLIP["ws"])
+    clip(norm=CLIP["ws"], out=False)
+    clip(norm=CLIP["out a"], given=CLIP["given"], ws=None)
+
+
+def test_a_workspace_on_tensors():
+    need = fftconv.load().fftconv_workspace_bytes_clip_grads((ctypes.c_int64 * 2)(100, 30), 2)
+    assert need >= 16
+    for name, size in (("a", 400), ("b", 60), ("out a", 400), ("out b", 120)):
+        for at in (0, size // 8 * 8 - 8, 8 - need):
+            clip(ws=CLIP[name] + at)
+            if not name.startswith("out"):
+                clip(ws=CLIP[name] + at, out=False)

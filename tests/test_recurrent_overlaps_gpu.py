@@ -80,3 +80,28 @@ def test_scans_side_by_side(b, c, n, dtype):
     assert lib.fftconv_gated_scan_backward(*where, b, c, n, 0, code, ws.data_ptr(), stream) == 0
     for got, want in ((du_, d[0]), (dw_, d[1]), (dv_, d[2]), (dstate_, dstate), (dy_, dy), (u_, u), (w_, w), (v_, v), (kept_, kept), (dlast_, dlast), (lengths_, lengths)):
         assert torch.equal(got.view(want.dtype).view(want.shape), want)
+
+
+def test_clipping_by_a_norm_beside_the_gradients():
+    """A norm in a slot of the buffer that is written is refused and nothing changes; in the slot behind it, it is taken."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    flat = torch.randn(100003, generator=g, device="cuda")
+    norm = layers.grad_norm([flat])
+    was = flat.clone()
+    ts = [flat[:60000], flat[60000:100002]]
+    for at in (0, 59999, 60000, 100001):
+        with pytest.raises(fftconv.FFTConvError, match="overlaps"):
+            layers.clip_grads(ts, 1.0, norm=flat[at])
+    other = torch.full_like(flat, 7.0)
+    with pytest.raises(fftconv.FFTConvError, match="overlaps"):
+        layers.clip_grads([flat], 1.0, out=[other], norm=other[5])
+    assert torch.equal(flat, was) and bool((other == 7.0).all())
+    flat[100002] = norm
+    want = [t.clone() for t in ts]
+    layers.clip_grads(want, 1.0, norm=norm)
+    assert float(layers.clip_grads(ts, 1.0, norm=flat[100002])) == float(norm) == float(flat[100002])
+    assert all(torch.equal(a, b) for a, b in zip(ts, want)) and not torch.equal(ts[0], was[:60000])
+    # read alone, it may be anywhere
+    flat.copy_(was)
+    layers.clip_grads([flat], 2.0, out=[other], norm=flat[17:18].abs_())
+    assert torch.equal(other[17], torch.clamp(2.0 / (flat[17].double() + 1e-6), max=1.0).float() * flat[17])
