@@ -104,6 +104,9 @@ __global__ void __launch_bounds__(256) k_norm(const ClipArgs a)
     }
 }
 
+// A norm that came with the call, to where the call wants it.
+__global__ void k_given(const ClipArgs a) { *a.norm_out = *a.norm; }
+
 template <typename T, typename O> __device__ __forceinline__ void scale_piece(const void *in, void *out, int64_t first, int count, float by)
 {
     const T *const x = (const T *)in + first;
@@ -233,6 +236,12 @@ int clip_grads(const void *const *in, void *const *out, const int64_t *counts, c
             FC_HIP(hipGetLastError());
             a.count = 0, a.norm_out = nullptr;
         }
+    }
+    if (norm_in && norm && norm != norm_in) {
+        a.norm_out = norm;
+        k_given<<<1, 1, 0, s>>>(a);
+        FC_HIP(hipGetLastError());
+        a.norm_out = nullptr;
     }
     if (!out) return FFTCONV_OK;
     return each_launch(in, out, counts, types, types_out, tensors, true, [&](const Tensors &t, uint32_t groups) -> int {
