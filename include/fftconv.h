@@ -361,7 +361,7 @@ int fftconv_linear_f8(const uint8_t *x, const float *x_scale, const uint8_t *w, 
  *   grads[i]; apart from that nothing that is written (results, norm, workspace) overlaps anything else, a norm that is given among it (refused, as
  *   is one tensor twice in place).  dtypes_out[i]: that of grads[i], or fp32; NULL: those of grads.  Squares are added in 64 bits, c is rounded
  *   to fp32, products are rounded to their type.  In place and with c = 1 nothing is written.  Where a gradient is NaN, norm is NaN and so is
- *   everything; where one is infinite, norm is, and c = 0.
+ *   everything; where one is infinite, norm is, and c = 0.  An infinite max_norm clips nothing: c = 1 by an infinite norm too.
  *   norm: where not NULL, the norm goes there as fp32, or the one that was given.  norm_in: NULL, or a norm (one fp32 on the device) that is taken
  *   instead: that of several devices' gradients, say.  workspace: fftconv_workspace_bytes_clip_grads bytes (NULL will do with norm_in). */
 size_t fftconv_workspace_bytes_clip_grads(const int64_t *counts, int64_t tensors);

@@ -131,7 +131,8 @@ __global__ void __launch_bounds__(256) k_clip(const Tensors t, const ClipArgs a)
     const double norm = a.norm ? (double)*a.norm : a.count ? norm_of(a.sums, a.count) : *a.total;
     if (a.norm_out && blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
     const double c = a.limit / (norm + a.eps);
-    const float by = c > 1.0 ? 1.f : (float)c;   // (a norm that is no number makes everything so)
+    const bool all = isinf(a.limit) && !isnan(norm);                 // (by an infinite norm the quotient is no number, and there is nothing to clip)
+    const float by = c > 1.0 || all ? 1.f : (float)c;                // (a norm that is no number makes everything so)
     each_piece<true>(t, [&](int i, int64_t first, int count) {
         const int type = t.type[i] & 3;
         const bool wide = t.type[i] >> 2 == FFTCONV_F32;

@@ -38,3 +38,26 @@ def test_the_norm_goes_where_the_call_says(sizes):
     assert float(given) == 12.5
     for t, o in zip(grads, out):
         assert torch.equal(o, t * torch.tensor(1.0 / (12.5 + 1e-6), device="cuda", dtype=torch.float64).float())
+
+
+def test_limits_without_bound():
+    """A limit of infinity clips nothing, whatever the norm: c = 1, and only what is NaN makes everything NaN. (Its quotient by an infinite norm is no number.)"""
+    inf, nan = float("inf"), float("nan")
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        for bad in (None, inf, -inf, nan):
+            grads = [torch.arange(-50.0, 50.0, device="cuda").to(dtype), torch.ones(9000, device="cuda", dtype=dtype)]
+            if bad is not None:
+                grads[1][8999] = bad
+            out = [torch.empty_like(t) for t in grads]
+            norm = layers.clip_grads(grads, inf, out=out)
+            inside = [t.clone() for t in grads]
+            assert torch.equal(layers.clip_grads(inside, inf).nan_to_num(nan=-1.0), norm.nan_to_num(nan=-1.0))
+            for ts in (out, inside):
+                if bad is nan or bad != bad:
+                    assert torch.isnan(norm) and all(torch.isnan(t).all() for t in ts)
+                else:
+                    assert all(torch.equal(a, b) for a, b in zip(ts, grads))
+            assert bad is None or bad != bad or torch.isinf(norm)
+    # an infinite norm and a limit that is one: nothing but zeros, and NaN where the infinity was
+    t = torch.tensor([3.0, inf], device="cuda")
+    assert torch.isinf(layers.clip_grads([t], 3e38)) and t[0] == 0 and torch.isnan(t[1])
