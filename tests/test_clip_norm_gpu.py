@@ -61,3 +61,29 @@ def test_limits_without_bound():
     # an infinite norm and a limit that is one: nothing but zeros, and NaN where the infinity was
     t = torch.tensor([3.0, inf], device="cuda")
     assert torch.isinf(layers.clip_grads([t], 3e38)) and t[0] == 0 and torch.isnan(t[1])
+
+
+@pytest.mark.parametrize("into", [True, False])
+def test_a_norm_that_comes_with_the_call_is_taken_and_returned(into):
+    """Not the gradients' own: the factor is that of the given one, which comes back as it was, the same tensor; gradients change only in place."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    grads = [torch.randn(s, generator=g, device="cuda") for s in (4097, 12, 70001)]
+    was = [t.clone() for t in grads]
+    own = float(layers.grad_norm(grads))
+    given = torch.full((), 4 * own, device="cuda")
+    out = [torch.empty_like(t) for t in grads] if into else None
+    back = layers.clip_grads(grads, own, out=out, norm=given)
+    assert back is given and float(given) == float(torch.tensor(4 * own))
+    factor = torch.tensor(own / (float(given) + 1e-6), dtype=torch.float64).float().cuda()
+    for t, w in zip(out if into else grads, was):
+        assert torch.equal(t, w * factor)
+    if into:
+        assert all(torch.equal(a, b) for a, b in zip(grads, was))
+
+
+def test_results_elsewhere_leave_the_gradients_alone():
+    t = torch.tensor([3.0, 4.0], device="cuda")
+    out = torch.empty(2, device="cuda")
+    for limit, eps in ((5.0, 0.0), (2.5, 0.0), (0.0, 1e-6), (float("inf"), 1e-6), (1e-30, 1e-6)):
+        layers.clip_grads([t], limit, out=[out], eps=eps)
+        assert t.tolist() == [3.0, 4.0]
