@@ -6,7 +6,7 @@
 //
 // Bound by bytes: a first pass reads, a second reads again and writes, last pieces first, for what the first read last is still in the memory-side cache.
 // Where the factor is one, what would be written in place is left alone. Measured: 604 million values, 403 million of them bf16, the rest fp32, into fp32:
-// 285 us (5.7 TB/s) and 800 (4.8 to 5.0, half of it stores); stores past the cache in whole lines give the next call's first pass 30 us and lose 5. A dozen
+// 285 to 292 us (5.5 to 5.7 TB/s) and 800 (5.0, more than half of it stores); stores past the cache in whole lines give the next call's first pass 30 us and lose 5. A dozen
 // tensors of 1.9 MB together: 4.2 and 4.7 us, the call on the host 20.
 #include <cstdlib>
 

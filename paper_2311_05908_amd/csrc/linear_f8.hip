@@ -10,7 +10,8 @@
 // Which kernel: up to 64 tokens k_f8_few, bound by the weight's bytes, but for very long rows and very many outputs. Above, with k in pieces of 16 bytes (both operands aligned to them), k_f8_large on
 // tiles of 256 x 256 where these fill the compute units, else k_f8_small on 128 x 128 where there are 128 of those, or with k in ranges where there
 // are fewer and k is 1024 or more. Rows of other lengths are laid out again for these where that pays (f8_padded); everything else is k_f8's, which
-// takes any k at any alignment.
+// takes any k at any alignment: among it fewer than 128 tiles with a k below 1024 (768 -> 768: 65 tokens 6.9 us, 1024 7.2, 2688 8.4, and 9.1 for 2689, from where on
+// it is k_f8_small's; 768 -> 2304: 300 7.3, 896 8.6; a call takes 8 on the host; other kernels have not been tried there).
 #include "layers_index.h"
 #include "linear_common.h"
 
@@ -66,10 +67,11 @@ __device__ __forceinline__ bf16x8 widened(uint32_t lo, uint32_t hi)
     const bf16x8 v = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     return v;
 }
-// What the products of e4m3 keep: of eight neighbours along k, each down to 2^-13 of the largest one's power of two, then sums in fp32 (so does the
-// instruction for any of the 8-bit formats; measured with one product of 2^16 and one of 2^16 down to 2^-9 beside it). On normally distributed values that is
-// 1.3e-5 of the result: for results in 16 bits, whose own rounding is 2e-4 and more, of no account; fp32 results take the values to bf16, which
-// holds them, and bf16's products, which are exact, at half the rate.
+// What the products of e4m3 keep: of eight neighbours along k, each down to 2^-13 of the largest one's power of two (by the operands' exponents), the rest dropped,
+// then sums in fp32 (so does the instruction for any of the 8-bit formats; measured with one product of 2^16 and one of 2^16 down to 2^-9 beside it; sums
+// computed so round to the kernels' results). That is 1.3e-5 of the result on normally distributed values, 3.3e-5 with one channel in a hundred twenty times
+// as large: for results in 16 bits, whose own rounding is 2e-4 and more, of no account (one bf16 result in fifty is rounded the other way, one of fp16 in eight).
+// fp32 results take the values to bf16, which holds them, and bf16's products, which are exact, at half the rate: 8192 x 4096 -> 16384 1142 us instead of 567.
 template <bool CLOSE> __device__ __forceinline__ void product_of(const Half &r, const Half &s, f32x16 &c)
 {
     if constexpr (!CLOSE) {
